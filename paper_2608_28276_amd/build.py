@@ -16,13 +16,17 @@ import shutil
 import subprocess
 import sys
 import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libpask.so")
-KERNEL_SOURCES = ("pask_append.hip", "pask_attn.hip")   # persisting entries; reading them
+# Persisting entries and reading them; the same for latents, absorbed and expanded attention.
+KERNEL_SOURCES = ("pask_append.hip", "pask_attn.hip", "pask_latent.hip", "pask_latent_attn.hip",
+                  "pask_latent_prompt.hip")
+HOST_SOURCES = ("pask_api.cpp", "pask_latent_api.cpp")
 # The benchmark's on-device bandwidth probes: a library of their own, outside the C ABI.
 PROBE_LIB = os.path.join(PKG, "libpask_probe.so")
 
@@ -44,12 +48,13 @@ def _run(cmd):
 def build(verbose: bool = False) -> str:
     """Compile and link libpask.so; returns its path."""
     with tempfile.TemporaryDirectory(prefix="pask_build_") as tmp:
-        objs = []
-        for src in KERNEL_SOURCES:
-            objs.append(os.path.join(tmp, src.replace(".hip", ".o")))
-            _run([HIPCC, *COMMON, *DEVICE, "-c", os.path.join(CSRC, src), "-o", objs[-1]])
-        objs.append(os.path.join(tmp, "pask_api.o"))
-        _run([HIPCC, *COMMON, "-c", os.path.join(CSRC, "pask_api.cpp"), "-o", objs[-1]])
+        objs, cmds = [], []
+        for src in KERNEL_SOURCES + HOST_SOURCES:
+            objs.append(os.path.join(tmp, os.path.splitext(src)[0] + ".o"))
+            device = DEVICE if src in KERNEL_SOURCES else []
+            cmds.append([HIPCC, *COMMON, *device, "-c", os.path.join(CSRC, src), "-o", objs[-1]])
+        with ThreadPoolExecutor(4) as pool:
+            list(pool.map(_run, cmds))
         tmp_lib = os.path.join(tmp, "libpask.so")
         _run([HIPCC, *DEVICE, "-shared", "-fPIC", *objs, "-o", tmp_lib])
         shutil.move(tmp_lib, LIB)

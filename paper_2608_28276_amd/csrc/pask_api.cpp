@@ -3,26 +3,24 @@
 // before the first HIP call of an entry point.
 #include <math.h>
 #include <stdint.h>
-#include <stdio.h>
-#include <stdlib.h>
 #include <string.h>
 
 #include <algorithm>
-#include <atomic>
 #include <vector>
 
 #include <hip/hip_runtime_api.h>
 
+#include "pask_host.h"
 #include "pask_internal.h"
 
 namespace {
 
 using pask::CacheView;
 
-constexpr uint64_t kAlignSmall = 256;
-constexpr uint64_t kAlignPool = 4096;
-
-uint64_t align_up(uint64_t x, uint64_t a) { return (x + a - 1) / a * a; }
+using pask::align_up;
+using pask::aligned;
+using pask::column_of;
+using pask::kAlignSmall;
 
 bool valid_geom(const pask_geom* g) {
   if (!g) return false;
@@ -42,117 +40,32 @@ bool valid_geom(const pask_geom* g) {
   return true;
 }
 
+pask::CacheDims dims_of(const pask_geom* g) {
+  const uint64_t D = (uint64_t)g->head_dim, H = (uint64_t)g->n_kv_heads;
+  return pask::CacheDims{g->max_batch, g->n_layers, g->max_tokens_per_seq, g->recent_window, g->hi_pages, g->lo_pages,
+                         H * 2 * PASK_PAGE_TOKENS * D * 2,
+                         H * 2 * (PASK_PAGE_TOKENS * (D / 2) + PASK_PAGE_TOKENS * (D / PASK_QGROUP) * 2)};
+}
+
 // Layout of a cache buffer; false when the geometry is unsupported.
 bool layout_of(const pask_geom* g, pask_cache_layout* L) {
   if (!valid_geom(g)) return false;
-  memset(L, 0, sizeof(*L));
-  const uint64_t B = (uint64_t)g->max_batch, NL = (uint64_t)g->n_layers;
-  const uint64_t D = (uint64_t)g->head_dim, H = (uint64_t)g->n_kv_heads;
-  const uint64_t T = (uint64_t)g->max_tokens_per_seq;
-  const uint64_t W = (uint64_t)g->recent_window;
-  L->max_pages = (int32_t)((T + PASK_PAGE_TOKENS - 1) / PASK_PAGE_TOKENS);
-  L->counter_stride = pask::kCounterStride;
-  L->ring_pages = (int32_t)(B * NL * ((W + PASK_PAGE_TOKENS - 1) / PASK_PAGE_TOKENS));
-  L->staging_stride = (int32_t)(T + W + 4);
-  L->hi_page_bytes = H * 2 * PASK_PAGE_TOKENS * D * 2;
-  L->lo_page_bytes = H * 2 * (PASK_PAGE_TOKENS * (D / 2) + PASK_PAGE_TOKENS * (D / PASK_QGROUP) * 2);
-  uint64_t off = 0;
-  L->status_off = off;
-  off = align_up(off + 16, kAlignSmall);
-  L->counters_off = off;
-  off = align_up(off + B * NL * pask::kCounterStride * 4, kAlignSmall);
-  L->block_table_off = off;
-  off = align_up(off + B * NL * 2 * (uint64_t)L->max_pages * 4, kAlignSmall);
-  L->index_list_off = off;
-  off = align_up(off + B * NL * 2 * T * 4, kAlignSmall);
-  L->staging_off = off;
-  off = align_up(off + B * (uint64_t)L->staging_stride * 4, kAlignSmall);
-  L->budget_off = off;
-  off = align_up(off + sizeof(pask::BudgetTable), kAlignSmall);
-  L->ring_act_off = off;
-  off = align_up(off + B * NL * W, kAlignPool);
-  L->hi_pool_off = off;
-  off = align_up(off + ((uint64_t)L->ring_pages + g->hi_pages) * L->hi_page_bytes, kAlignPool);
-  L->lo_pool_off = off;
-  off = align_up(off + (uint64_t)g->lo_pages * L->lo_page_bytes, kAlignPool);
-  L->total_bytes = off;
+  *L = pask::layout_regions(dims_of(g));
   return true;
 }
 
 CacheView view_of(const pask_cache* c) {
-  pask_cache_layout L;
-  layout_of(&c->geom, &L);
-  uint8_t* base = static_cast<uint8_t*>(c->base);
-  CacheView v;
-  v.status = reinterpret_cast<uint32_t*>(base + L.status_off);
-  v.counters = reinterpret_cast<int32_t*>(base + L.counters_off);
-  v.block_table = reinterpret_cast<int32_t*>(base + L.block_table_off);
-  v.index_list = reinterpret_cast<int32_t*>(base + L.index_list_off);
-  v.staging = reinterpret_cast<int32_t*>(base + L.staging_off);
-  v.budget = reinterpret_cast<pask::BudgetTable*>(base + L.budget_off);
-  v.ring_act = base + L.ring_act_off;
-  v.hi_pool = base + L.hi_pool_off;
-  v.lo_pool = base + L.lo_pool_off;
-  v.n_layers = c->geom.n_layers;
+  const pask::CacheDims d = dims_of(&c->geom);
+  CacheView v = pask::view_regions(c->base, pask::layout_regions(d), d);
   v.n_kv_heads = c->geom.n_kv_heads;
   v.head_dim = c->geom.head_dim;
-  v.max_tokens = c->geom.max_tokens_per_seq;
-  v.max_pages = L.max_pages;
-  v.hi_pages = L.ring_pages + c->geom.hi_pages;
-  v.hi_base = L.ring_pages;
-  v.window = c->geom.recent_window;
-  v.ring_pp = (c->geom.recent_window + PASK_PAGE_TOKENS - 1) / PASK_PAGE_TOKENS;
-  v.staging_stride = L.staging_stride;
-  v.lo_pages = c->geom.lo_pages;
-  v.hi_page_bytes = (uint32_t)L.hi_page_bytes;
-  v.lo_page_bytes = (uint32_t)L.lo_page_bytes;
   return v;
 }
 
-bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
-
-// PASK_DEBUG set to anything but "" or "0" when the library is first used
-// turns on a check after every entry point that launches kernels: it waits for
-// the stream, turns a launch or execution error into PASK_E_HIP, and writes to
-// stderr the entry point with the HIP error, or with the cache's device status
-// flags when they differ from the last ones reported.  A failure is then named
-// by the call that caused it, not by a later synchronisation.  Calls on a
-// stream that is being captured into a graph are not checked.  Off by default:
-// each check costs a host round trip.
-bool debug_on() {
-  static const bool on = [] {
-    const char* e = getenv("PASK_DEBUG");
-    return e && e[0] && strcmp(e, "0") != 0;
-  }();
-  return on;
-}
-
 int debug_check(const char* where, int st, const pask_cache* const* caches, int n_caches, hipStream_t stream) {
-  if (st != PASK_OK || !debug_on()) return st;
-  hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
-  hipError_t e = hipStreamIsCapturing(stream, &cs);
-  if (e == hipSuccess && cs != hipStreamCaptureStatusNone) return st;
-  if (e == hipSuccess) e = hipStreamSynchronize(stream);
-  if (e == hipSuccess) e = hipGetLastError();
-  if (e != hipSuccess) {
-    fprintf(stderr, "pask: %s: %s\n", where, hipGetErrorString(e));
-    return PASK_E_HIP;
-  }
-  static std::atomic<uint32_t> reported{0};
-  for (int i = 0; i < n_caches; ++i) {
-    pask_cache_layout L;
-    layout_of(&caches[i]->geom, &L);
-    uint32_t word = 0;
-    const uint8_t* status = static_cast<const uint8_t*>(caches[i]->base) + L.status_off;
-    if (hipMemcpyAsync(&word, status, sizeof(word), hipMemcpyDeviceToHost, stream) != hipSuccess ||
-        hipStreamSynchronize(stream) != hipSuccess) {
-      fprintf(stderr, "pask: %s: status word not readable\n", where);
-      return PASK_E_HIP;
-    }
-    if (word != 0 && reported.exchange(word) != word)
-      fprintf(stderr, "pask: %s: device status flags 0x%x\n", where, word);
-  }
-  return st;
+  const void* words[2];
+  for (int i = 0; i < n_caches; ++i) words[i] = caches[i]->base;   // the status word opens the buffer
+  return pask::debug_check_words(where, st, words, n_caches, stream);
 }
 
 int debug_check(const char* where, int st, const pask_cache* cache, hipStream_t stream) {
@@ -170,15 +83,10 @@ int check_cache(const pask_cache* c) {
 }
 
 int check_policy(const pask_policy* p, const pask_cache* c) {
-  if (!p) return PASK_E_ARG;
-  if (p->n_tags < 1 || p->n_tags > PASK_MAX_TAGS || p->n_groups < 1 || p->n_groups > PASK_MAX_GROUPS)
-    return PASK_E_POLICY;
-  if ((int32_t)p->n_layers != c->geom.n_layers) return PASK_E_SHAPE;
+  const int st = pask::check_policy_layers(p, c->geom.n_layers);
+  if (st != PASK_OK) return st;
   if ((int32_t)p->recent_window != c->geom.recent_window) return PASK_E_SHAPE;
-  for (uint32_t l = 0; l < p->n_layers; ++l)
-    if (p->group_of_layer[l] >= p->n_groups) return PASK_E_POLICY;
-  if (p->n_states > PASK_MAX_STATES) return PASK_E_POLICY;
-  return PASK_OK;
+  return pask::check_policy_groups(p);
 }
 
 // Bytes one token persists in the layers of group c under action a (the
@@ -190,20 +98,6 @@ void group_costs(const pask_policy* p, const pask_geom& g, int64_t m[PASK_MAX_GR
   for (uint32_t l = 0; l < p->n_layers; ++l) ++layers[p->group_of_layer[l]];
   for (int c = 0; c < PASK_MAX_GROUPS; ++c)
     for (int a = 0; a < 3; ++a) m[c][a] = layers[c] * entry[a];
-}
-
-pask::TableColumn column_of(const pask_policy* p, int layer) {
-  pask::TableColumn t;
-  memset(&t, 0, sizeof(t));
-  const int c = p->group_of_layer[layer];
-  for (uint32_t z = 0; z < p->n_tags; ++z) {
-    t.a0[z] = p->action[z][c];
-    t.amin[z] = p->floor_[z][c];
-  }
-  t.n_tags = p->n_tags;
-  t.n_sink = p->n_sink;
-  t.group = (uint32_t)c;
-  return t;
 }
 
 uint32_t fnv1a32(const uint8_t* d, size_t n) {

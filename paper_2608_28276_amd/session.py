@@ -10,7 +10,7 @@ import struct
 
 import torch
 
-from . import pask
+from . import latent, pask
 
 # The current stream's raw handle: building torch's Stream object costs 2 us of
 # a call's 10.6.  Not in torch's public interface: a torch without it goes the
@@ -214,3 +214,136 @@ class PaskSession:
         vs = r[:, :, 16 * D + 32 * NG:].copy().view(np.uint16).reshape(-1, H, 16, NG)
         fix = lambda a: a.transpose(0, 2, 1, 3).reshape(-1, H, a.shape[-1])[:n]
         return fix(kc), fix(ks).astype(np.int64), fix(vc), fix(vs).astype(np.int64)
+
+
+class PaskLatentSession:
+    """One latent cache of `max_batch` sequences x `n_layers` layers on one GPU,
+    its workspace and its calls (include/pask_latent.h).  Calls run on the
+    current stream of the session's device and are ordered there; tensors are
+    checked for type, shape, device and contiguity."""
+
+    def __init__(self, policy_blob: bytes, *, max_batch: int, n_layers: int, n_q_heads: int, rank: int, rope_dim: int,
+                 max_tokens_per_seq: int, hi_pages: int, lo_pages: int, softmax_scale: float,
+                 max_ctx_hint: int | None = None, device: str = "cuda:0", extra_bytes: int = 0,
+                 prefill: int | None = None):
+        self.device = torch.device(device)
+        if self.device.index is None:
+            self.device = torch.device(self.device.type, torch.cuda.current_device())
+        self.geom = latent.make_latent_geom(max_batch=max_batch, n_layers=n_layers, n_q_heads=n_q_heads, rank=rank,
+                                            rope_dim=rope_dim, max_tokens_per_seq=max_tokens_per_seq,
+                                            hi_pages=hi_pages, lo_pages=lo_pages)
+        self.policy = pask.pask_policy_load(policy_blob, None)
+        if self.policy.recent_window:
+            raise pask.PaskError(pask.PASK_E_UNSUPPORTED, "PaskLatentSession: a policy with a recent window")
+        if self.policy.n_layers != n_layers:
+            raise pask.PaskError(pask.PASK_E_SHAPE, "PaskLatentSession: the policy's layers")
+        self.nbytes = latent.pask_latent_cache_bytes(self.geom)
+        if self.nbytes == 0:
+            raise pask.PaskError(pask.PASK_E_SHAPE, "pask_latent_cache_bytes")
+        self.layout = latent.pask_latent_cache_layout_query(self.geom)
+        self.softmax_scale = float(softmax_scale)
+        self.max_ctx_hint = max_ctx_hint or max_tokens_per_seq
+        self.ws_bytes = latent.pask_latent_workspace_bytes(self.geom, max_batch, self.max_ctx_hint)
+        # extra_bytes, prefill: as in PaskSession
+        self.buf = torch.empty(self.nbytes + extra_bytes, dtype=torch.uint8, device=self.device)
+        self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=self.device)
+        if prefill is not None:
+            self.buf.fill_(prefill)
+            self.ws.fill_(prefill)
+        self.cache = latent.pask_latent_cache()
+        self._call(latent.pask_latent_cache_init, self.cache, self.geom, self.buf, self.nbytes)
+
+    def _call(self, f, *args):
+        """f(*args, stream) with the session's device current."""
+        index = self.device.index
+        if torch.cuda.current_device() == index:
+            return f(*args, self.stream)
+        with torch.cuda.device(index):
+            return f(*args, self.stream)
+
+    @property
+    def stream(self) -> int:
+        if _raw_stream is None:
+            return torch.cuda.current_stream(self.device).cuda_stream
+        return _raw_stream(self.device.index)
+
+    def _bf16(self, name, t, *shape):
+        latent.check_tensor(name, t, torch.bfloat16, shape, self.device)
+
+    # -- the calls ---------------------------------------------------------
+    def append(self, layer: int, tags, c, r, n_new=None, keep_all: bool = False):
+        """c bf16 [batch, max_new, rank], r bf16 [batch, max_new, rope_dim], tags uint8 [batch, max_new] (None with
+        keep_all), n_new int32 [batch] or None."""
+        g = self.geom
+        self._bf16("c", c, None, None, g.rank)
+        b, m = c.shape[:2]
+        self._bf16("r", r, b, m, g.rope_dim)
+        if tags is not None:
+            latent.check_tensor("tags", tags, torch.uint8, (b, m), self.device)
+        if n_new is not None:
+            latent.check_tensor("n_new", n_new, torch.int32, (b,), self.device)
+        if m == 0:
+            return
+        self._call(latent.pask_latent_append, self.policy, self.cache, layer, b, n_new, m, tags, c, r,
+                   pask.PASK_APPEND_KEEP_ALL if keep_all else 0)
+
+    def read(self, layer: int, c_out, r_out, pos_out, cu_out):
+        """The persisted entries of the first cu_out.shape[0] - 1 sequences as dense rows: c_out bf16 [rows, rank],
+        r_out bf16 [rows, rope_dim], pos_out int32 [rows] or None, cu_out int32 [batch + 1]."""
+        g = self.geom
+        self._bf16("c_out", c_out, None, g.rank)
+        rows = c_out.shape[0]
+        self._bf16("r_out", r_out, rows, g.rope_dim)
+        if pos_out is not None:
+            latent.check_tensor("pos_out", pos_out, torch.int32, (rows,), self.device)
+        latent.check_tensor("cu_out", cu_out, torch.int32, (None,), self.device)
+        self._call(latent.pask_latent_read, self.cache, layer, cu_out.shape[0] - 1, rows, c_out, r_out, pos_out, cu_out)
+
+    def decode(self, layer: int, q, out, lse=None, tags_new=None, c_new=None, r_new=None,
+               max_ctx_hint: int | None = None):
+        """q bf16 [batch, heads, rank + rope_dim], out bf16 [batch, heads, rank], lse fp32 [batch, heads] or None; with
+        tags_new uint8 [batch], c_new bf16 [batch, rank] and r_new bf16 [batch, rope_dim], one token per sequence is
+        persisted first."""
+        g = self.geom
+        self._bf16("q", q, None, g.n_q_heads, g.rank + g.rope_dim)
+        b = q.shape[0]
+        self._bf16("out", out, b, g.n_q_heads, g.rank)
+        if lse is not None:
+            latent.check_tensor("lse", lse, torch.float32, (b, g.n_q_heads), self.device)
+        if tags_new is not None:
+            latent.check_tensor("tags_new", tags_new, torch.uint8, (b,), self.device)
+            self._bf16("c_new", c_new, b, g.rank)
+            self._bf16("r_new", r_new, b, g.rope_dim)
+        self._call(latent.pask_latent_decode_attn, self.policy, self.cache, layer, b, q, out, lse, tags_new, c_new,
+                   r_new, self.softmax_scale, max_ctx_hint or self.max_ctx_hint, self.ws, self.ws_bytes)
+
+    def prompt(self, q, kv, r, out, lse, cu_q, cu_k, max_q: int):
+        """latent.prompt_attn with the session's softmax scale."""
+        latent.prompt_attn(q, kv, r, out, lse, cu_q, cu_k, max_q, self.softmax_scale)
+
+    def reset(self):
+        self._call(latent.pask_latent_cache_reset, self.cache)
+
+    def stats(self, batch: int | None = None):
+        """(stats, status) of the first `batch` sequences; synchronises the stream."""
+        return self._call(latent.pask_latent_cache_stats, self.policy, self.cache, batch or self.geom.max_batch)
+
+    # -- going back, as after a rejected draft --------------------------------
+    def _head(self):
+        return self.buf[:self.layout.block_table_off]
+
+    def save(self):
+        """The state of every sequence and layer as it is now, for restore(): the counts, cursors and flags (pages are
+        only added to, and what lies past the counts is written again before it is read)."""
+        return self._head().clone()
+
+    def restore(self, saved):
+        """Back to the state save() returned, on the same stream; void after a reset() in between."""
+        self._head().copy_(saved)
+
+    # -- views of the cache buffer (inspection) -----------------------------
+    def counters(self):
+        """int32 [max_batch, n_layers, 8]: n_hi, n_lo, n_pos, n_drop, n_forced, n_lost, ..."""
+        g, off = self.geom, self.layout.counters_off
+        n = g.max_batch * g.n_layers * self.layout.counter_stride
+        return self.buf[off:off + 4 * n].view(torch.int32).view(g.max_batch, g.n_layers, self.layout.counter_stride)
