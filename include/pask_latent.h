@@ -176,7 +176,7 @@ int pask_latent_decode_attn(const pask_policy* policy, pask_latent_cache* cache,
  * Errors: PASK_E_ARG (null or misaligned pointers: q_dev, kv_dev, r_dev,
  * out_dev 16 bytes, the others 4; a negative size; softmax_scale not finite),
  * PASK_E_SHAPE (unsupported dimensions, or batch * n_heads *
- * ceil(min(max_q, total_q) / 128) of 2^24 or more),
+ * ceil(max_q / (64 if max_q <= 64 else 256)) of 2^23 or more),
  * PASK_E_HIP.  With max_q or total_q 0 nothing is done; with total_k 0 the
  * pointers of keys are not read. */
 int pask_latent_prompt_attn(int32_t batch, int32_t n_heads, int32_t nope_dim, int32_t rope_dim, int32_t v_dim,

@@ -273,7 +273,7 @@ int pask_latent_prompt_attn(int32_t batch, int32_t n_heads, int32_t nope_dim, in
   a.max_q = std::min(max_q, total_q);
   a.total_q = total_q;
   a.total_k = total_k;
-  if (pask::latent_prompt_blocks(a) > (1 << 24) - 1) return PASK_E_SHAPE;   // a launch holds 2^32 - 1 threads
+  if (pask::latent_prompt_blocks(a) > (1 << 23) - 1) return PASK_E_SHAPE;   // a launch holds 2^32 - 1 threads
   const hipError_t e = pask::launch_latent_prompt(a, stream);
   return pask::debug_check_words("pask_latent_prompt_attn", e == hipSuccess ? PASK_OK : PASK_E_HIP, nullptr, 0, stream);
 }
