@@ -12,6 +12,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "pask_latent_device.h"
 
@@ -19,7 +20,6 @@ namespace pask {
 namespace {
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
-typedef short s16x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256, kWaves = 4;           // of the merge
@@ -32,23 +32,6 @@ __device__ __forceinline__ f32x4_t mfma(uint4 a, uint4 b, f32x4_t c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0,
                                                  0, 0);
 }
-
-// Four 2-byte elements of one column from 4 rows of 16 elements: of each 16
-// lanes, lanes 4r .. 4r + 3 address row r's four 8-byte quarters, and lane i
-// receives element i of the rows.
-__device__ __forceinline__ uint2 read_transposed(const uint8_t* lds) {
-  typedef __attribute__((address_space(3))) s16x4_t lds_s16x4;
-  return __builtin_bit_cast(
-      uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(__attribute__((address_space(3))) uint8_t*)lds));
-}
-
-// 16 bytes per lane from memory straight into LDS: lane l's to lds + 16 l (lds is
-// the same for the wave).  The caller waits (wait_loads) and synchronises.
-__device__ __forceinline__ void load_to_lds(const uint8_t* src, uint8_t* lds) {
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)src,
-                                   (__attribute__((address_space(3))) uint32_t*)lds, 16, 0, 2);   // 2: non-temporal
-}
-__device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0F70); }   // vmcnt(0)
 
 // ---------------------------------------------------------------------------
 // the list of tiles
@@ -136,7 +119,7 @@ struct Tile {
 #pragma unroll
     for (int k = 0; k < (2 * PG::KI + T / 64 - 1) / (T / 64); ++k) {
       const int x = wave + k * (T / 64);
-      if (x < n) load_to_lds((x < PG::KI ? b0 : b1) + x * 1024 + lane * 16, tile + x * 1024);
+      if (x < n) load_to_lds<true>((x < PG::KI ? b0 : b1) + x * 1024 + lane * 16, tile + x * 1024);
     }
   }
   // Slots from n on as zeros: what lies there is not an entry (any bytes, NaN
@@ -216,16 +199,18 @@ __global__ __launch_bounds__(64 * latent_waves(NHT), 2) void latent_attn_kernel(
   using PG = LatentPage<R, P>;
   constexpr int NW = latent_waves(NHT), T = 64 * NW;
   constexpr int KI = PG::KI, DT = R / (16 * NW);   // score steps; 16-element output tiles of a wave
-  __shared__ __align__(16) uint8_t s_tile[2][2 * PG::kHiBytes];
-  __shared__ uint4 s_p[NHT * 64];
-  __shared__ float s_alpha[NHT * 16];
-  __shared__ int s_grown[NHT];
-  __shared__ long long s_scan[NW + 2];
+  __shared__ __align__(16) struct {
+    uint8_t tile[2][2 * PG::kHiBytes];
+    uint4 p[NHT * 64];
+    long long scan[NW + 2];
+    float alpha[NHT * 16];
+    int grown[NHT];
+  } sm;
   const CacheView& cv = a.cv;
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int q4 = lane >> 4, n = lane & 15;
   long long units = 1;
-  const ListPlace place = find_in_list<T>(a, s_scan, [&](long long total) {
+  const ListPlace place = find_in_list<T>(a, sm.scan, [&](long long total) {
     units = (total + a.workers - 1) / a.workers;
     return (long long)blockIdx.x * units;
   });
@@ -268,13 +253,13 @@ __global__ __launch_bounds__(64 * latent_waves(NHT), 2) void latent_attn_kernel(
   long long start = place.start;                   // the list's tile 0 of sequence s
   int j = (int)(u0 - start), buf = 0;
   load_queries(s.b);
-  fetch(s, j, s_tile[0]);
-  if (j >= s.nt_hi && s.slots(j) > 0) low.store_low(s_tile[0], s.slots(j));
+  fetch(s, j, sm.tile[0]);
+  if (j >= s.nt_hi && s.slots(j) > 0) low.store_low(sm.tile[0], s.slots(j));
   wait_loads();
   __syncthreads();
   for (long long u = u0; u < u1; ++u) {
-    uint8_t* tile = s_tile[buf];
-    uint8_t* other = s_tile[buf ^ 1];
+    uint8_t* tile = sm.tile[buf];
+    uint8_t* other = sm.tile[buf ^ 1];
     const int m = s.slots(j);
     const bool ends = j + 1 == s.nt || u + 1 == u1;             // the worker's last tile of this sequence
     Seq next = s;
@@ -286,7 +271,7 @@ __global__ __launch_bounds__(64 * latent_waves(NHT), 2) void latent_attn_kernel(
     if (u + 1 < u1) fetch(next, nj, other);
     if (m < kTile && (j < s.nt_hi || m <= 0)) {    // a HIGH store's last tile, or an empty sequence's
       Tile<R, P, T>::clear_from(tile, m);
-      __syncthreads();
+      lds_barrier();
     }
     if (wave < NHT) {
       f32x4_t s0 = {0.0f, 0.0f, 0.0f, 0.0f}, s1 = s0;
@@ -315,34 +300,41 @@ __global__ __launch_bounds__(64 * latent_waves(NHT), 2) void latent_attn_kernel(
         part += x[r];
       }
       sum = sum * alpha + part;
-      s_p[wave * 64 + lane] = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
+      sm.p[wave * 64 + lane] = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
                                          pack_bf16x2(x[6], x[7]));
-      if (q4 == 0) s_alpha[wave * 16 + n] = alpha;
+      if (q4 == 0) sm.alpha[wave * 16 + n] = alpha;
       const bool grown = __ballot(alpha != 1.0f) != 0ull;
-      if (lane == 0) s_grown[wave] = grown;
+      if (lane == 0) sm.grown[wave] = grown;
     }
-    __syncthreads();
+    lds_barrier();
     int grown = 0;
 #pragma unroll
-    for (int h = 0; h < NHT; ++h) grown |= s_grown[h];
+    for (int h = 0; h < NHT; ++h) grown |= sm.grown[h];
     if (__builtin_amdgcn_readfirstlane(grown)) {
 #pragma unroll
       for (int h = 0; h < NHT; ++h) {
-        const float alpha = s_alpha[h * 16 + n];
+        const float alpha = sm.alpha[h * 16 + n];
 #pragma unroll
         for (int d = 0; d < DT; ++d) acc[h][d] *= alpha;
       }
     }
     uint4 pf[NHT];
 #pragma unroll
-    for (int h = 0; h < NHT; ++h) pf[h] = s_p[h * 64 + lane];
+    for (int h = 0; h < NHT; ++h) pf[h] = sm.p[h * 64 + lane];
+    const uint32_t vs = lds_address(tile) + v_at;
+    auto add_values = [&](auto first) {            // output tiles first .. + 3 (those below DT)
+      constexpr int d0 = decltype(first)::value, k = d0 * 512;
+      constexpr int k1 = DT > d0 + 1 ? k + 512 : k, k2 = DT > d0 + 2 ? k + 1024 : k, k3 = DT > d0 + 3 ? k + 1536 : k;
+      uint4 v[4];
+      read_transposed<k, k1, k2, k3, PG::kHiBytes>(vs, vs, vs, vs, v);
 #pragma unroll
-    for (int d = 0; d < DT; ++d) {
-      const uint2 v0 = read_transposed(tile + v_at + d * 512), v1 = read_transposed(tile + v_at + d * 512 + PG::kHiBytes);
-      const uint4 v = make_uint4(v0.x, v0.y, v1.x, v1.y);
+      for (int d = 0; d < 4; ++d)
 #pragma unroll
-      for (int h = 0; h < NHT; ++h) acc[h][d] = mfma(v, pf[h], acc[h][d]);
-    }
+        for (int h = 0; h < NHT; ++h)
+          if (d0 + d < DT) acc[h][d0 + d] = mfma(v[d], pf[h], acc[h][d0 + d]);
+    };
+    add_values(std::integral_constant<int, 0>{});
+    if constexpr (DT > 4) add_values(std::integral_constant<int, 4>{});
     if (u + 1 < u1 && nj >= next.nt_hi && next.slots(nj) > 0) low.store_low(other, next.slots(nj));
 
     if (ends) {
@@ -354,13 +346,13 @@ __global__ __launch_bounds__(64 * latent_waves(NHT), 2) void latent_attn_kernel(
         a.ws_seq[2 * s.b] = part;
         a.ws_seq[2 * s.b + 1] = whole ? 0 : (int)((start + s.nt - 1) / units) - (int)blockIdx.x + 1;
       }
-      __syncthreads();                             // s_alpha has been read
+      lds_barrier();                               // the scale factors have been read
       if (wave < NHT) {
         sum += __shfl_xor(sum, 16);
         sum += __shfl_xor(sum, 32);
         const int head = wave * 16 + n;
         if (q4 == 0) {
-          s_alpha[head] = sum == 0.0f ? 0.0f : 1.0f / sum;
+          sm.alpha[head] = sum == 0.0f ? 0.0f : 1.0f / sum;
           if (whole) {
             if (a.lse && head < a.heads)
               a.lse[(size_t)s.b * a.heads + head] =
@@ -373,12 +365,12 @@ __global__ __launch_bounds__(64 * latent_waves(NHT), 2) void latent_attn_kernel(
         }
       }
       if (u + 1 < u1) load_queries(next.b);
-      __syncthreads();
+      lds_barrier();
 #pragma unroll
       for (int h = 0; h < NHT; ++h) {
         const int head = h * 16 + n;
         if (head < a.heads) {
-          const float inv = s_alpha[head];
+          const float inv = sm.alpha[head];
 #pragma unroll
           for (int d = 0; d < DT; ++d) {
             const int dim = 16 * (wave * DT + d) + 4 * q4;

@@ -1,6 +1,6 @@
 // Shared by the latent-attention kernels (pask_latent.hip: persisting and
-// reading back; pask_latent_attn.hip: absorbed decode attention): the launch
-// arguments and the page layout.
+// reading back; pask_latent_attn.hip: absorbed decode attention;
+// pask_latent_prompt.hip: expanded attention): the page layout and LDS access.
 #pragma once
 
 #include "pask_device.h"
@@ -45,6 +45,59 @@ __device__ __forceinline__ uint4 low_values(uint32_t w, float s) {
                     pack_bf16x2(v(hi, 0), v(hi, 1)), pack_bf16x2(v(hi, 2), v(hi, 3)));
 }
 __device__ __forceinline__ float half_value(uint16_t h) { return (float)__builtin_bit_cast(_Float16, h); }
+
+// Transposing reads of LDS (ds_read_b64_tr_b16): of each 16 lanes, lanes 4r ..
+// 4r + 3 address row r's four 8-byte quarters (4 rows of 16 2-byte elements),
+// and lane i receives element i of the rows.  Four pairs of reads at a time,
+// pair k at at[k] + kOff[k] and kStep behind it, in one asm block that waits
+// for its own reads: before the builtin the compiler waits for every copy into
+// LDS under way (load_to_lds), which is what the copies are there to avoid.
+template <int kOff0, int kOff1, int kOff2, int kOff3, int kStep>
+__device__ __forceinline__ void read_transposed(uint32_t at0, uint32_t at1, uint32_t at2, uint32_t at3, uint4 (&v)[4]) {
+  uint2 a[4], b[4];
+  asm volatile(
+      "ds_read_b64_tr_b16 %0, %8 offset:%12\n\t"
+      "ds_read_b64_tr_b16 %1, %8 offset:%13\n\t"
+      "ds_read_b64_tr_b16 %2, %9 offset:%14\n\t"
+      "ds_read_b64_tr_b16 %3, %9 offset:%15\n\t"
+      "ds_read_b64_tr_b16 %4, %10 offset:%16\n\t"
+      "ds_read_b64_tr_b16 %5, %10 offset:%17\n\t"
+      "ds_read_b64_tr_b16 %6, %11 offset:%18\n\t"
+      "ds_read_b64_tr_b16 %7, %11 offset:%19\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(a[0]), "=&v"(b[0]), "=&v"(a[1]), "=&v"(b[1]), "=&v"(a[2]), "=&v"(b[2]), "=&v"(a[3]), "=&v"(b[3])
+      : "v"(at0), "v"(at1), "v"(at2), "v"(at3), "n"(kOff0), "n"(kOff0 + kStep), "n"(kOff1), "n"(kOff1 + kStep),
+        "n"(kOff2), "n"(kOff2 + kStep), "n"(kOff3), "n"(kOff3 + kStep)
+      : "memory");
+#pragma unroll
+  for (int k = 0; k < 4; ++k) v[k] = make_uint4(a[k].x, a[k].y, b[k].x, b[k].y);
+}
+// A barrier that LDS reads and writes of the workgroup are ordered by, and that
+// copies under way do not wait for (__syncthreads waits for them).
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xC07F);              // lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+__device__ __forceinline__ uint4 read_lds16(uint32_t lds) {
+  typedef __attribute__((address_space(3))) u32x4_t lds_u32x4;
+  const u32x4_t x = *(const lds_u32x4*)(uintptr_t)lds;
+  return make_uint4(x[0], x[1], x[2], x[3]);
+}
+__device__ __forceinline__ uint32_t lds_address(const uint8_t* p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint8_t*)p;
+}
+
+// 16 bytes per lane from memory straight into LDS: lane l's to lds + 16 l (lds is
+// the same for the wave).  The caller waits (wait_loads) and synchronises.
+// kOnce: data read once per call (non-temporal).
+template <bool kOnce>
+__device__ __forceinline__ void load_to_lds(const void* src, uint8_t* lds) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)src,
+                                   (__attribute__((address_space(3))) uint32_t*)lds, 16, 0, kOnce ? 2 : 0);
+}
+__device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0F70); }   // vmcnt(0)
 
 }  // namespace
 }  // namespace pask

@@ -8,17 +8,21 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "pask_device.h"
-#include "pask_latent_internal.h"
+#include "pask_latent_device.h"
 
 namespace pask {
 namespace {
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
-typedef short s16x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
 constexpr int kKeys = 64;                          // keys of a step
+// The reference of a query's weights moves only when a score exceeds it by more
+// than this (in base 2).  Weights up to 2^60 and their sums are as precise as
+// weights below 1 (bf16 and fp32 have the same exponents), and stay far from the
+// largest fp32; a reference that follows every maximum costs a multiplication of
+// all sums in the loop, which the compiler answers with copies of them.
+constexpr float kHeadroom = 60.0f;
 constexpr float kLn2 = 0.6931471805599453f;
 
 // D[32x32] += A[32x16] B[16x32]: lane l holds A[l % 32][8 (l / 32) ..], B[8 (l / 32) ..][l % 32], and
@@ -27,13 +31,6 @@ __device__ __forceinline__ f32x16_t mfma(uint4 a, uint4 b, f32x16_t c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0,
                                                  0, 0);
 }
-// Element i of four rows for lane i of each 16 (lanes 4r .. 4r + 3 address row r's 8-byte quarters).
-__device__ __forceinline__ uint2 read_transposed(const uint8_t* lds) {
-  typedef __attribute__((address_space(3))) s16x4_t lds_s16x4;
-  return __builtin_bit_cast(
-      uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(__attribute__((address_space(3))) uint8_t*)lds));
-}
-
 // Rows of C 16-byte chunks in LDS, row t's chunk d at t * C + swap(t, d): the
 // operand reads, 8 neighbouring rows' chunk d at once, fall on all banks
 // (256 / (16 C) rows share the 64 banks).
@@ -43,23 +40,23 @@ __device__ __forceinline__ int key_swap(int t, int d) { return d ^ ((C >= 16 ? t
 template <int C>
 __device__ __forceinline__ int value_swap(int t, int d) { return d ^ ((t & (C / 2 - 1)) << 1); }
 
-// O += P V key by key, for a step in which a value that some query does not
-// see is infinite or NaN (a weight of 0 times it is not 0): only keys up to
-// `see` are added.  Lane (g, n) holds the weights of query n for half of the
-// keys, lane (1 - g, n) the others'; the weights move down one register a turn.
+// O += P V key by key over 32 keys (values at s_v), where a value that some
+// query does not see is infinite or NaN (a weight of 0 times it is not 0): only
+// keys up to `see` are added.  Lane (g, n) holds the weights of query n for half
+// of the keys, lane (1 - g, n) the others'; the weights move down one register
+// a turn.
 template <int VT, int VC>
-__device__ __forceinline__ void add_seen_values(const uint8_t* s_v, f32x16_t (&s)[2], f32x16_t (&o)[VT], int see, int g,
-                                             int n) {
+__device__ __forceinline__ void add_seen_values(const uint8_t* s_v, f32x16_t s, f32x16_t (&o)[VT], int see, int g, int n) {
 #pragma unroll 1
-  for (int x = 0; x < 32; ++x) {
+  for (int x = 0; x < 16; ++x) {
     asm volatile("" : "+v"(g));                    // no code: keeps this rare path's addresses out of the loops around it
-    const float mine = s[0][0];
+    const float mine = s[0];
 #pragma unroll
-    for (int r = 0; r < 31; ++r) s[r >> 4][r & 15] = s[(r + 1) >> 4][(r + 1) & 15];
+    for (int r = 0; r < 15; ++r) s[r] = s[r + 1];
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
       const float p = __shfl(mine, n + 32 * w);
-      const int t = 32 * (x >> 4) + 8 * ((x & 15) >> 2) + 4 * w + (x & 3);
+      const int t = 8 * (x >> 2) + 4 * w + (x & 3);
       if (t > see) continue;
 #pragma unroll
       for (int m = 0; m < VT; ++m)
@@ -76,34 +73,29 @@ __device__ __forceinline__ void add_seen_values(const uint8_t* s_v, f32x16_t (&s
   }
 }
 
-// 16 bytes per lane from memory straight into LDS: lane l's to lds + 16 l (lds is
-// the same for the wave).  The caller waits (wait_loads) and synchronises.
-__device__ __forceinline__ void load_to_lds(const uint16_t* src, uint8_t* lds) {
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)src,
-                                   (__attribute__((address_space(3))) uint32_t*)lds, 16, 0, 0);
-}
-__device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0F70); }   // vmcnt(0)
-
 // A workgroup of W waves takes 32 W queries of one head (32 per wave) through
-// the keys they see, 64 at a time:
+// the keys they see, 64 at a step, 32 at a time:
 //   scores  S^T = K Q^T on v_mfma_f32_32x32x16_bf16: a lane holds scores of one
 //           query, so its softmax needs one exchange (with the lane 32 on);
 //   weights online softmax in base 2, rounded to bf16 (2^-8 of a weight at
-//           most, as the values' own); the reference maximum moves only when
-//           exceeded by more than 8, sums are kept of the unrounded weights;
+//           most, as the values' own); sums are kept of the unrounded weights;
 //   values  O^T += V^T P^T: the scores' lane layout is the operand layout of P
-//           up to the order of the 16 keys of a step, which the value operand
+//           up to the order of the 16 keys of a product, which the value operand
 //           follows (two transposing reads of 4 keys).
-// The next step's keys and values are on their way into the other LDS buffers
-// meanwhile.  Rows past the sequence repeat its last one: no query sees them.
+// The scores of the next 32 keys are computed beside the weights of the current
+// ones, so that the matrix and the vector units work at once; two steps of keys
+// and values are on their way into a ring of three LDS buffers meanwhile.
+// Rows past the sequence repeat its last one: no query sees them.
 template <int N, int P, int V, int W>
 __global__ __launch_bounds__(64 * W, 2) void latent_prompt_kernel(LatentPromptArgs a, int q_tiles) {
   constexpr int T = 64 * W, kRows = 32 * W;
   constexpr int NC = N / 8, PC = P / 8, VC = V / 8, VT = V / 32;   // 16-byte chunks of a row; output tiles
   constexpr int NI = N / 16, KI = (N + P) / 16;                    // score steps
-  constexpr int kKn = kKeys * NC * 16, kKr = kKeys * PC * 16, kV = kKeys * VC * 16;
-  __shared__ __align__(16) uint8_t s_kv[2][kKn + kKr + kV];
-  __shared__ int s_wild;
+  constexpr int kKn = kKeys * NC * 16, kKr = kKeys * PC * 16, kV = kKeys * VC * 16, kStep = kKn + kKr + kV;
+  __shared__ __align__(1024) struct {
+    uint8_t kv[3][kStep];
+    int wild;                                      // some value of the step is infinite or NaN
+  } sm;
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int g = lane >> 5, n = lane & 31;
   const int head = (int)blockIdx.x % a.heads, rest = (int)blockIdx.x / a.heads;
@@ -117,6 +109,7 @@ __global__ __launch_bounds__(64 * W, 2) void latent_prompt_kernel(LatentPromptAr
   const int last = min(tile * kRows + kRows, nq_in) - 1;       // the tile's last query
   const int n_see = min(nk, last + past + 1);                  // keys it sees; may be <= 0
   const int steps = n_see > 0 ? (n_see + kKeys - 1) / kKeys : 0;
+  const int whole = min(steps, max(0, (tile * kRows + past + 1) / kKeys));   // steps that every query sees whole
 
   // Scores are scaled by |scale|; its sign goes to the queries, so that a score's maximum is a scaled one's.
   uint4 qf[KI];
@@ -132,26 +125,28 @@ __global__ __launch_bounds__(64 * W, 2) void latent_prompt_kernel(LatentPromptAr
   const size_t kv_row = (size_t)a.heads * (N + V);
   const uint16_t* kv = a.kv + ((size_t)k0 * a.heads + head) * (N + V);
   const uint16_t* rk = a.r + (size_t)k0 * P;
-  auto fetch = [&](int j, uint8_t* dst) {          // keys 64 j .. of the sequence
+  // Rows of C chunks, `stride` elements apart, of keys 64 j .. into LDS, a wave taking every W-th KiB; the offset from
+  // the step's first row is the lane's own for the whole call.
+  auto fetch_rows = [&](auto chunks, auto swap, const uint16_t* src, uint32_t stride, int j, uint8_t* dst) {
+    constexpr int C = decltype(chunks)::value;
+    src += (size_t)j * kKeys * stride;
+    const int most = nk - 1 - j * kKeys;
 #pragma unroll
-    for (int k = 0; k < (NC + W - 1) / W; ++k) {
-      const int x = wave + k * W, c = x * 64 + lane, t = c / NC;
-      if (x < NC)
-        load_to_lds(kv + min(j * kKeys + t, nk - 1) * kv_row + 8 * key_swap<NC>(t, c % NC), dst + x * 1024);
+    for (int k = 0; k < (C + W - 1) / W; ++k) {
+      const int x = wave + k * W, c = x * 64 + lane, t = c / C;
+      if ((k + 1) * W > C && x >= C) continue;
+      const uint32_t at = (uint32_t)(most < kKeys - 1 ? min(t, most) : t) * stride + 8 * swap(t, c % C);
+      load_to_lds<false>(src + at, dst + x * 1024);
     }
-#pragma unroll
-    for (int k = 0; k < (PC + W - 1) / W; ++k) {
-      const int x = wave + k * W, c = x * 64 + lane, t = c / PC;
-      if (x < PC)
-        load_to_lds(rk + (size_t)min(j * kKeys + t, nk - 1) * P + 8 * key_swap<PC>(t, c % PC), dst + kKn + x * 1024);
-    }
-#pragma unroll
-    for (int k = 0; k < (VC + W - 1) / W; ++k) {
-      const int x = wave + k * W, c = x * 64 + lane, t = c / VC;
-      if (x < VC)
-        load_to_lds(kv + min(j * kKeys + t, nk - 1) * kv_row + N + 8 * value_swap<VC>(t, c % VC),
-                    dst + kKn + kKr + x * 1024);
-    }
+  };
+  auto fetch = [&](int j) {
+    if (j >= steps) return;
+    uint8_t* dst = sm.kv[j % 3];
+    fetch_rows(std::integral_constant<int, NC>{}, [](int t, int d) { return key_swap<NC>(t, d); }, kv, (uint32_t)kv_row, j,
+               dst);
+    fetch_rows(std::integral_constant<int, PC>{}, [](int t, int d) { return key_swap<PC>(t, d); }, rk, P, j, dst + kKn);
+    fetch_rows(std::integral_constant<int, VC>{}, [](int t, int d) { return value_swap<VC>(t, d); }, kv + N,
+               (uint32_t)kv_row, j, dst + kKn + kKr);
   };
   f32x16_t o[VT];
 #pragma unroll
@@ -159,111 +154,157 @@ __global__ __launch_bounds__(64 * W, 2) void latent_prompt_kernel(LatentPromptAr
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[m][r] = 0.0f;
   float mx = -INFINITY, sum = 0.0f;                // the reference (of scaled scores), the weights' sum
-  const int l16 = lane & 15, half = (lane >> 4) & 1;           // value operand: 4 keys x 16 elements per 16 lanes
-  if (steps > 0) fetch(0, s_kv[0]);
-  wait_loads();
-  __syncthreads();
-  // One step of the wave.  kEdge: some query of the wave does not see all its keys.
-  auto attend = [&](auto edge_tag, int j, const uint8_t* s_k, bool wild) {
-    constexpr bool kEdge = decltype(edge_tag)::value;
-    const uint8_t* s_v = s_k + kKn + kKr;
-    const int see = row + past - j * kKeys;        // this query sees the step's keys 0 .. see
-    auto key_at = [&](int i, int u) {              // operand i of keys 32 u ..
-      const int t = 32 * u + n;
-      return *reinterpret_cast<const uint4*>(i < NI ? s_k + (t * NC + key_swap<NC>(t, 2 * i + g)) * 16
-                                                    : s_k + kKn + (t * PC + key_swap<PC>(t, 2 * (i - NI) + g)) * 16);
-    };
-    f32x16_t s[2];
+  // Operand addresses.  The swaps XOR a chunk's index with bits of its row, so chunk d + x of a lane's row, x and d
+  // having no bit in common, is at (the address of chunk d) ^ 16 x: one base each for the per-head keys, the rotary
+  // keys and the values.
+  const int l16 = lane & 15, v_row = 4 * g + (l16 >> 2);       // value operand: 4 keys x 16 elements per 16 lanes
+  const uint32_t kn_at = (uint32_t)(n * NC + key_swap<NC>(n, g)) * 16;
+  const uint32_t kr_at = (uint32_t)(kKn + (n * PC + key_swap<PC>(n, g)) * 16);
+  const uint32_t v_at = (uint32_t)(kKn + kKr + (v_row * VC + value_swap<VC>(v_row, 2 * ((lane >> 4) & 1) + ((l16 & 3) >> 1))) * 16 +
+                                   8 * (l16 & 1));
+  auto fresh = [](uint32_t x) {                    // no code: addresses are made where they are used, not kept in registers
+    asm volatile("" : "+v"(x));
+    return x;
+  };
+  auto scores = [&](uint32_t kvs, int u) {         // of keys 32 u .. of the step at LDS address kvs
+    f32x16_t s;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) s[0][r] = s[1][r] = 0.0f;
-    uint4 kf[2][2] = {{key_at(0, 0), key_at(0, 1)}, {key_at(1, 0), key_at(1, 1)}};
+    for (int r = 0; r < 16; ++r) s[r] = 0.0f;
+    const uint32_t kn = fresh(kvs + kn_at), kr = fresh(kvs + kr_at);
 #pragma unroll
     for (int i = 0; i < KI; ++i) {
-      const uint4 c0 = kf[i & 1][0], c1 = kf[i & 1][1];
-      s[0] = mfma(c0, qf[i], s[0]);
-      s[1] = mfma(c1, qf[i], s[1]);
-      if (i + 2 < KI) {
-        kf[i & 1][0] = key_at(i + 2, 0);
-        kf[i & 1][1] = key_at(i + 2, 1);
-      }
+      const uint32_t at = i < NI ? (kn ^ (32 * i)) + u * 32 * NC * 16 : (kr ^ (32 * (i - NI))) + u * 32 * PC * 16;
+      s = mfma(read_lds16(at), qf[i], s);
     }
-    if constexpr (kEdge) {
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[u][r] = 32 * u + 8 * (r >> 2) + 4 * g + (r & 3) <= see ? s[u][r] : -INFINITY;
-    }
-    float top = -INFINITY;
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) top = fmaxf(top, s[u][r]);
-    top = fmaxf(top, __shfl_xor(top, 32));
-    top = top == -INFINITY ? top : top * scale;
-    const float ref = top > mx + 8.0f ? top : mx;
-    if (__ballot(ref != mx)) {
-      const float alpha = ref == mx ? 1.0f : __builtin_amdgcn_exp2f(mx - ref);
-      sum *= alpha;
-#pragma unroll
-      for (int m = 0; m < VT; ++m) o[m] *= alpha;
-      mx = ref;
-    }
-    const float base = mx == -INFINITY ? 0.0f : mx;
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        float w = __builtin_amdgcn_exp2f(fmaf(s[u][r], scale, -base));
-        if constexpr (kEdge) w = 32 * u + 8 * (r >> 2) + 4 * g + (r & 3) <= see ? w : 0.0f;
-        s[u][r] = w;
-        sum += w;
-      }
-    if constexpr (kEdge) {
-      if (wild) {
-        add_seen_values<VT, VC>(s_v, s, o, see, g, n);
-        return;
-      }
-    }
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {                // 16 keys
-        const uint4 p =
-            make_uint4(pack_bf16x2(s[u][8 * h], s[u][8 * h + 1]), pack_bf16x2(s[u][8 * h + 2], s[u][8 * h + 3]),
-                       pack_bf16x2(s[u][8 * h + 4], s[u][8 * h + 5]), pack_bf16x2(s[u][8 * h + 6], s[u][8 * h + 7]));
-#pragma unroll
-        for (int m = 0; m < VT; ++m) {
-          uint2 w[2];
-#pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            const int t = 32 * u + 16 * h + 8 * x + 4 * g + (l16 >> 2);
-            const int d = 4 * m + 2 * half + ((l16 & 3) >> 1);
-            w[x] = read_transposed(s_v + (t * VC + value_swap<VC>(t, d)) * 16 + 8 * (l16 & 1));
-          }
-          o[m] = mfma(make_uint4(w[0].x, w[0].y, w[1].x, w[1].y), p, o[m]);
-        }
-      }
+    return s;
   };
-  // Steps that every query of the workgroup sees whole, then those at the edge.
-  const int whole = min(steps, max(0, (tile * kRows + past + 1) / kKeys));
-  for (int j = 0; j < whole; ++j) {
-    if (j + 1 < steps) fetch(j + 1, s_kv[(j + 1) & 1]);
-    attend(std::false_type{}, j, s_kv[j & 1], false);
-    wait_loads();
-    __syncthreads();
+  auto highest = [&](const f32x16_t& s) {          // of the lane's query, scaled
+    float top = fmaxf(s[0], s[1]);
+#pragma unroll
+    for (int r = 2; r < 16; ++r) top = fmaxf(top, s[r]);
+    top = fmaxf(top, __shfl_xor(top, 32));
+    return top == -INFINITY ? top : top * scale;
+  };
+  auto exceeds = [&](float top) { return __ballot(top > mx + kHeadroom) != 0ull; };
+  auto refer = [&](float top) {                    // the reference follows a maximum that exceeds it
+    const float ref = top > mx + kHeadroom ? top : mx;
+    const float alpha = ref == mx ? 1.0f : __builtin_amdgcn_exp2f(mx - ref);
+    sum *= alpha;
+#pragma unroll
+    for (int m = 0; m < VT; ++m) o[m] *= alpha;
+    mx = ref;
+  };
+  auto weigh = [&](f32x16_t& s) {
+    const float base = mx == -INFINITY ? 0.0f : mx;
+    float part = 0.0f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale, -base));
+      if (r & 1) part += s[r];
+      else sum += s[r];
+    }
+    sum += part;
+  };
+  auto add_values = [&](uint32_t kvs, int u, const f32x16_t& s) {
+    const uint32_t vs = fresh(kvs + v_at + u * 32 * VC * 16);
+    uint4 p[2], v[4];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)                    // 16 keys
+      p[h] = make_uint4(pack_bf16x2(s[8 * h], s[8 * h + 1]), pack_bf16x2(s[8 * h + 2], s[8 * h + 3]),
+                        pack_bf16x2(s[8 * h + 4], s[8 * h + 5]), pack_bf16x2(s[8 * h + 6], s[8 * h + 7]));
+    constexpr int kRow = VC * 16, k1 = 16 * kRow;
+    if constexpr (VT == 4) {
+      read_transposed<0, 0, 0, 0, 8 * kRow>(vs, vs ^ 64, vs ^ 128, vs ^ 192, v);
+#pragma unroll
+      for (int m = 0; m < 4; ++m) o[m] = mfma(v[m], p[0], o[m]);
+      read_transposed<k1, k1, k1, k1, 8 * kRow>(vs, vs ^ 64, vs ^ 128, vs ^ 192, v);
+#pragma unroll
+      for (int m = 0; m < 4; ++m) o[m] = mfma(v[m], p[1], o[m]);
+    } else {
+      read_transposed<0, 0, k1, k1, 8 * kRow>(vs, vs ^ 64, vs, vs ^ 64, v);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) o[x & 1] = mfma(v[x], p[x >> 1], o[x & 1]);
+    }
+  };
+
+  fetch(0);
+  fetch(1);
+  wait_loads();
+  __syncthreads();
+  // The steps that every query sees whole, in units of 32 keys: unit i's scores s become weights beside the scores of
+  // unit i + 1.  The loop is left to move the reference: in it the sums are only added to.
+  f32x16_t s;
+  const int units = 2 * whole;
+  auto step_of = [&](int i) { return lds_address(sm.kv[(i >> 1) % 3]); };
+  if (units > 0) {
+    s = scores(step_of(0), 0);
+    refer(highest(s));
   }
+  for (int i = 0; i < units;) {
+    float top = -INFINITY;
+    bool out = false;
+    for (; i + 1 < units && !out; ++i) {
+      f32x16_t next = scores(step_of(i + 1), (i + 1) & 1);
+      weigh(s);
+      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+#pragma unroll
+      for (int k = 0; k < KI; ++k) {               // a product, an operand's read, a part of the weights
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, (40 + KI - 1) / KI, 0);
+        __builtin_amdgcn_sched_group_barrier(0x400, (16 + KI - 1) / KI, 0);
+      }
+      add_values(step_of(i), i & 1, s);
+      s = next;
+      top = highest(s);
+      out = exceeds(top);
+      if ((i & 1) == 0) {                          // step i / 2 + 1 is next: its copies have arrived
+        wait_loads();
+        __syncthreads();
+        fetch(i / 2 + 2);
+      }
+    }
+    if (out) {
+      refer(top);
+    } else {                                       // the last unit
+      weigh(s);
+      add_values(step_of(i), 1, s);
+      ++i;
+    }
+  }
+  wait_loads();
+  __syncthreads();
+  // Steps at the edge: some query of the workgroup does not see all their keys.
   for (int j = whole; j < steps; ++j) {
-    const uint8_t* s_k = s_kv[j & 1];
-    if (j + 1 < steps) fetch(j + 1, s_kv[(j + 1) & 1]);
+    const uint8_t* kvs = sm.kv[j % 3];
+    fetch(j + 2);
     // Values that are infinite or NaN, where some query may not see them.
-    if (threadIdx.x == 0) s_wild = 0;
-    __syncthreads();
+    if (threadIdx.x == 0) sm.wild = 0;
+    lds_barrier();
     bool wild = false;
     for (int c = (int)threadIdx.x; c < kKeys * VC; c += T)
-      wild |= abs_max_bits8(reinterpret_cast<const uint4*>(s_k + kKn + kKr)[c]) >= 0x7F80u;
-    if (wild) s_wild = 1;
-    __syncthreads();
-    if (row0 + 31 + past >= j * kKeys) attend(std::true_type{}, j, s_k, s_wild != 0);   // some query of the wave sees a key
+      wild |= abs_max_bits8(reinterpret_cast<const uint4*>(kvs + kKn + kKr)[c]) >= 0x7F80u;
+    if (wild) sm.wild = 1;
+    lds_barrier();
+#pragma unroll 1
+    for (int u = 0; u < 2; ++u) {
+      if (row0 + 31 + past < j * kKeys + 32 * u) break;        // no query of the wave sees a key
+      const int see = row + past - j * kKeys - 32 * u;         // this query sees the unit's keys 0 .. see
+      auto hidden = [&](int r) { return 8 * (r >> 2) + 4 * g + (r & 3) > see; };
+      s = scores(lds_address(kvs), u);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = hidden(r) ? -INFINITY : s[r];
+      refer(highest(s));
+      const float base = mx == -INFINITY ? 0.0f : mx;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float w = __builtin_amdgcn_exp2f(fmaf(s[r], scale, -base));
+        s[r] = hidden(r) ? 0.0f : w;
+        sum += s[r];
+      }
+      if (sm.wild) add_seen_values<VT, VC>(kvs + kKn + kKr + u * 32 * VC * 16, s, o, see, g, n);
+      else add_values(lds_address(kvs), u, s);
+    }
     wait_loads();
     __syncthreads();
   }
