@@ -23,6 +23,7 @@ constexpr int kKeys = 64;                          // keys of a step
 // largest fp32; a reference that follows every maximum costs a multiplication of
 // all sums in the loop, which the compiler answers with copies of them.
 constexpr float kHeadroom = 60.0f;
+constexpr int kAhead = 4;                          // score operands read ahead of their product
 constexpr float kLn2 = 0.6931471805599453f;
 
 // D[32x32] += A[32x16] B[16x32]: lane l holds A[l % 32][8 (l / 32) ..], B[8 (l / 32) ..][l % 32], and
@@ -205,13 +206,14 @@ __global__ __launch_bounds__(64 * W, 2) void latent_prompt_kernel(LatentPromptAr
     }
     sum += part;
   };
+  auto packed = [](const f32x16_t& s, int h) {     // weights of 16 keys as an operand
+    return make_uint4(pack_bf16x2(s[8 * h], s[8 * h + 1]), pack_bf16x2(s[8 * h + 2], s[8 * h + 3]),
+                      pack_bf16x2(s[8 * h + 4], s[8 * h + 5]), pack_bf16x2(s[8 * h + 6], s[8 * h + 7]));
+  };
   auto add_values = [&](uint32_t kvs, int u, const f32x16_t& s) {
     const uint32_t vs = fresh(kvs + v_at + u * 32 * VC * 16);
-    uint4 p[2], v[4];
-#pragma unroll
-    for (int h = 0; h < 2; ++h)                    // 16 keys
-      p[h] = make_uint4(pack_bf16x2(s[8 * h], s[8 * h + 1]), pack_bf16x2(s[8 * h + 2], s[8 * h + 3]),
-                        pack_bf16x2(s[8 * h + 4], s[8 * h + 5]), pack_bf16x2(s[8 * h + 6], s[8 * h + 7]));
+    const uint4 p[2] = {packed(s, 0), packed(s, 1)};
+    uint4 v[4];
     constexpr int kRow = VC * 16, k1 = 16 * kRow;
     if constexpr (VT == 4) {
       read_transposed<0, 0, 0, 0, 8 * kRow>(vs, vs ^ 64, vs ^ 128, vs ^ 192, v);
@@ -241,20 +243,53 @@ __global__ __launch_bounds__(64 * W, 2) void latent_prompt_kernel(LatentPromptAr
     refer(highest(s));
   }
   for (int i = 0; i < units;) {
-    float top = -INFINITY;
+    float top = -INFINITY, odd_sum = 0.0f;
+    const float base = mx == -INFINITY ? 0.0f : mx;
     bool out = false;
     for (; i + 1 < units && !out; ++i) {
-      f32x16_t next = scores(step_of(i + 1), (i + 1) & 1);
-      weigh(s);
-      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      const uint32_t nkvs = step_of(i + 1), nu = (i + 1) & 1;
+      const uint32_t kn = fresh(nkvs + kn_at + nu * 32 * NC * 16), kr = fresh(nkvs + kr_at + nu * 32 * PC * 16);
+      const uint32_t vs = fresh(step_of(i) + v_at + (i & 1) * 32 * VC * 16);
+      auto operand = [&](int k) { return read_lds16(k < NI ? kn ^ (32 * k) : kr ^ (32 * (k - NI))); };
+      constexpr int kRow = VC * 16, k1 = 16 * kRow;
+      f32x16_t next;
 #pragma unroll
-      for (int k = 0; k < KI; ++k) {               // a product, an operand's read, a part of the weights
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x002, (40 + KI - 1) / KI, 0);
-        __builtin_amdgcn_sched_group_barrier(0x400, (16 + KI - 1) / KI, 0);
+      for (int r = 0; r < 16; ++r) next[r] = 0.0f;
+      uint4 kf[kAhead], v[4], p = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) kf[k] = operand(k);
+      // Pinned order: a score product, the read of one to come, a part of the weights; from the middle on also a
+      // product of values with the first 16 weights.
+      constexpr int kWeigh = KI - 2, kFirst = kWeigh / 2;
+#pragma unroll
+      for (int k = 0; k < KI; ++k) {
+        next = mfma(kf[k % kAhead], qf[k], next);
+        if (k + kAhead < KI) kf[k % kAhead] = operand(k + kAhead);
+#pragma unroll
+        for (int r = 16 * k / kWeigh; r < min(16, 16 * (k + 1) / kWeigh); ++r) {
+          s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale, -base));
+          if (r & 1) odd_sum += s[r];
+          else sum += s[r];
+        }
+        if (VT == 4 && k >= kFirst && k < kFirst + 4) {
+          if (k == kFirst) {
+            p = packed(s, 0);
+            read_transposed<0, 0, 0, 0, 8 * kRow>(vs, vs ^ 64, vs ^ 128, vs ^ 192, v);
+          }
+          o[k - kFirst] = mfma(v[k - kFirst], p, o[k - kFirst]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
       }
-      add_values(step_of(i), i & 1, s);
+      if constexpr (VT == 4) {
+        p = packed(s, 1);
+        read_transposed<k1, k1, k1, k1, 8 * kRow>(vs, vs ^ 64, vs ^ 128, vs ^ 192, v);
+#pragma unroll
+        for (int m = 0; m < 4; ++m) o[m] = mfma(v[m], p, o[m]);
+      } else {
+        read_transposed<0, 0, k1, k1, 8 * kRow>(vs, vs ^ 64, vs, vs ^ 64, v);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) o[x & 1] = mfma(v[x], packed(s, x >> 1), o[x & 1]);
+      }
       s = next;
       top = highest(s);
       out = exceeds(top);
@@ -264,6 +299,7 @@ __global__ __launch_bounds__(64 * W, 2) void latent_prompt_kernel(LatentPromptAr
         fetch(i / 2 + 2);
       }
     }
+    sum += odd_sum;
     if (out) {
       refer(top);
     } else {                                       // the last unit
