@@ -93,13 +93,13 @@ __global__ __launch_bounds__(64 * W, 2) void latent_prompt_kernel(LatentPromptAr
   constexpr int NC = N / 8, PC = P / 8, VC = V / 8, VT = V / 32;   // 16-byte chunks of a row; output tiles
   constexpr int NI = N / 16, KI = (N + P) / 16;                    // score steps
   constexpr int kKn = kKeys * NC * 16, kKr = kKeys * PC * 16, kV = kKeys * VC * 16, kStep = kKn + kKr + kV;
-  __shared__ __align__(1024) struct {
-    uint8_t kv[3][kStep];
-    int wild;                                      // some value of the step is infinite or NaN
-  } sm;
+  __shared__ __align__(1024) uint8_t s_kv[3][kStep];
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int g = lane >> 5, n = lane & 31;
-  const int head = (int)blockIdx.x % a.heads, rest = (int)blockIdx.x / a.heads;
+  // Workgroups go to the 8 XCDs in turn.  With a multiple of 8 heads each XCD gets neighbouring heads.
+  int head = (int)blockIdx.x % a.heads;
+  const int rest = (int)blockIdx.x / a.heads;
+  if (a.heads % 8 == 0) head = head % 8 * (a.heads / 8) + head / 8;
   const int b = rest % a.batch, tile = q_tiles - 1 - rest / a.batch;   // the longest first
   const int q0 = min(max(a.cu_q[b], 0), a.total_q), q1 = min(max(a.cu_q[b + 1], 0), a.total_q);
   const int k0 = min(max(a.cu_k[b], 0), a.total_k), k1 = min(max(a.cu_k[b + 1], 0), a.total_k);
@@ -110,7 +110,6 @@ __global__ __launch_bounds__(64 * W, 2) void latent_prompt_kernel(LatentPromptAr
   const int last = min(tile * kRows + kRows, nq_in) - 1;       // the tile's last query
   const int n_see = min(nk, last + past + 1);                  // keys it sees; may be <= 0
   const int steps = n_see > 0 ? (n_see + kKeys - 1) / kKeys : 0;
-  const int whole = min(steps, max(0, (tile * kRows + past + 1) / kKeys));   // steps that every query sees whole
 
   // Scores are scaled by |scale|; its sign goes to the queries, so that a score's maximum is a scaled one's.
   uint4 qf[KI];
@@ -142,7 +141,7 @@ __global__ __launch_bounds__(64 * W, 2) void latent_prompt_kernel(LatentPromptAr
   };
   auto fetch = [&](int j) {
     if (j >= steps) return;
-    uint8_t* dst = sm.kv[j % 3];
+    uint8_t* dst = s_kv[j % 3];
     fetch_rows(std::integral_constant<int, NC>{}, [](int t, int d) { return key_swap<NC>(t, d); }, kv, (uint32_t)kv_row, j,
                dst);
     fetch_rows(std::integral_constant<int, PC>{}, [](int t, int d) { return key_swap<PC>(t, d); }, rk, P, j, dst + kKn);
@@ -233,116 +232,129 @@ __global__ __launch_bounds__(64 * W, 2) void latent_prompt_kernel(LatentPromptAr
   fetch(1);
   wait_loads();
   __syncthreads();
-  // The steps that every query sees whole, in units of 32 keys: unit i's scores s become weights beside the scores of
-  // unit i + 1.  The loop is left to move the reference: in it the sums are only added to.
+  // Units of 32 keys.  After a step's first unit the workgroup meets: the next
+  // step's copies have arrived, and the buffer of the step before is free for
+  // those of the step after next.
+  const int units = 2 * steps;
+  auto step_of = [&](int i) { return lds_address(s_kv[(i >> 1) % 3]); };
+  auto meet = [&](int i) {
+    if (i & 1) return;
+    wait_loads();
+    __syncthreads();
+    fetch(i / 2 + 2);
+  };
+  // The units that all queries of the wave see whole: unit i's scores s become
+  // weights beside the scores of unit i + 1.  The loop is left to move the
+  // reference: in it the sums are only added to.
+  const int whole = row0 < nq_in ? min(units, max(0, (row0 + past + 1) / 32)) : 0;
+  float base = 0.0f, odd_sum = 0.0f, top = -INFINITY;
+  auto turn = [&](int i, f32x16_t& s, f32x16_t& next) {
+    const uint32_t nkvs = step_of(i + 1), nu = (i + 1) & 1;
+    const uint32_t kn = fresh(nkvs + kn_at + nu * 32 * NC * 16), kr = fresh(nkvs + kr_at + nu * 32 * PC * 16);
+    const uint32_t vs = fresh(step_of(i) + v_at + (i & 1) * 32 * VC * 16);
+    auto operand = [&](int k) { return read_lds16(k < NI ? kn ^ (32 * k) : kr ^ (32 * (k - NI))); };
+    constexpr int kRow = VC * 16, k1 = 16 * kRow;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) next[r] = 0.0f;
+    uint4 kf[kAhead], v[4], p = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) kf[k] = operand(k);
+    // Pinned order: a score product, the read of one to come, a part of the weights; from the middle on also a
+    // product of values with the first 16 weights.
+    constexpr int kWeigh = KI - 2, kFirst = kWeigh / 2;
+#pragma unroll
+    for (int k = 0; k < KI; ++k) {
+      next = mfma(kf[k % kAhead], qf[k], next);
+      if (k + kAhead < KI) kf[k % kAhead] = operand(k + kAhead);
+#pragma unroll
+      for (int r = 16 * k / kWeigh; r < min(16, 16 * (k + 1) / kWeigh); ++r) {
+        s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale, -base));
+        if (r & 1) odd_sum += s[r];
+        else sum += s[r];
+      }
+      if (VT == 4 && k >= kFirst && k < kFirst + 4) {
+        if (k == kFirst) {
+          p = packed(s, 0);
+          read_transposed<0, 0, 0, 0, 8 * kRow>(vs, vs ^ 64, vs ^ 128, vs ^ 192, v);
+        }
+        o[k - kFirst] = mfma(v[k - kFirst], p, o[k - kFirst]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if constexpr (VT == 4) {
+      p = packed(s, 1);
+      read_transposed<k1, k1, k1, k1, 8 * kRow>(vs, vs ^ 64, vs ^ 128, vs ^ 192, v);
+#pragma unroll
+      for (int m = 0; m < 4; ++m) o[m] = mfma(v[m], p, o[m]);
+    } else {
+      read_transposed<0, 0, k1, k1, 8 * kRow>(vs, vs ^ 64, vs, vs ^ 64, v);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) o[x & 1] = mfma(v[x], packed(s, x >> 1), o[x & 1]);
+    }
+    top = highest(next);
+    meet(i);
+    return exceeds(top);
+  };
   f32x16_t s;
-  const int units = 2 * whole;
-  auto step_of = [&](int i) { return lds_address(sm.kv[(i >> 1) % 3]); };
-  if (units > 0) {
+  int i = 0;
+  if (whole > 0) {
     s = scores(step_of(0), 0);
     refer(highest(s));
   }
-  for (int i = 0; i < units;) {
-    float top = -INFINITY, odd_sum = 0.0f;
-    const float base = mx == -INFINITY ? 0.0f : mx;
+  while (i < whole) {
+    base = mx == -INFINITY ? 0.0f : mx;
+    f32x16_t t;
     bool out = false;
-    for (; i + 1 < units && !out; ++i) {
-      const uint32_t nkvs = step_of(i + 1), nu = (i + 1) & 1;
-      const uint32_t kn = fresh(nkvs + kn_at + nu * 32 * NC * 16), kr = fresh(nkvs + kr_at + nu * 32 * PC * 16);
-      const uint32_t vs = fresh(step_of(i) + v_at + (i & 1) * 32 * VC * 16);
-      auto operand = [&](int k) { return read_lds16(k < NI ? kn ^ (32 * k) : kr ^ (32 * (k - NI))); };
-      constexpr int kRow = VC * 16, k1 = 16 * kRow;
-      f32x16_t next;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) next[r] = 0.0f;
-      uint4 kf[kAhead], v[4], p = make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-      for (int k = 0; k < kAhead; ++k) kf[k] = operand(k);
-      // Pinned order: a score product, the read of one to come, a part of the weights; from the middle on also a
-      // product of values with the first 16 weights.
-      constexpr int kWeigh = KI - 2, kFirst = kWeigh / 2;
-#pragma unroll
-      for (int k = 0; k < KI; ++k) {
-        next = mfma(kf[k % kAhead], qf[k], next);
-        if (k + kAhead < KI) kf[k % kAhead] = operand(k + kAhead);
-#pragma unroll
-        for (int r = 16 * k / kWeigh; r < min(16, 16 * (k + 1) / kWeigh); ++r) {
-          s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale, -base));
-          if (r & 1) odd_sum += s[r];
-          else sum += s[r];
-        }
-        if (VT == 4 && k >= kFirst && k < kFirst + 4) {
-          if (k == kFirst) {
-            p = packed(s, 0);
-            read_transposed<0, 0, 0, 0, 8 * kRow>(vs, vs ^ 64, vs ^ 128, vs ^ 192, v);
-          }
-          o[k - kFirst] = mfma(v[k - kFirst], p, o[k - kFirst]);
-        }
-        __builtin_amdgcn_sched_barrier(0);
+    while (i + 2 < whole) {                        // two turns, so that neither's scores are copied
+      out = turn(i, s, t);
+      ++i;
+      if (out) {
+        s = t;
+        break;
       }
-      if constexpr (VT == 4) {
-        p = packed(s, 1);
-        read_transposed<k1, k1, k1, k1, 8 * kRow>(vs, vs ^ 64, vs ^ 128, vs ^ 192, v);
-#pragma unroll
-        for (int m = 0; m < 4; ++m) o[m] = mfma(v[m], p, o[m]);
-      } else {
-        read_transposed<0, 0, k1, k1, 8 * kRow>(vs, vs ^ 64, vs, vs ^ 64, v);
-#pragma unroll
-        for (int x = 0; x < 4; ++x) o[x & 1] = mfma(v[x], packed(s, x >> 1), o[x & 1]);
-      }
-      s = next;
-      top = highest(s);
-      out = exceeds(top);
-      if ((i & 1) == 0) {                          // step i / 2 + 1 is next: its copies have arrived
-        wait_loads();
-        __syncthreads();
-        fetch(i / 2 + 2);
-      }
+      out = turn(i, t, s);
+      ++i;
+      if (out) break;
+    }
+    if (!out && i + 1 < whole) {
+      out = turn(i, s, t);
+      ++i;
+      s = t;
     }
     sum += odd_sum;
+    odd_sum = 0.0f;
     if (out) {
       refer(top);
-    } else {                                       // the last unit
+    } else {                                       // the last of them
       weigh(s);
-      add_values(step_of(i), 1, s);
+      add_values(step_of(i), i & 1, s);
+      meet(i);
       ++i;
     }
   }
-  wait_loads();
-  __syncthreads();
-  // Steps at the edge: some query of the workgroup does not see all their keys.
-  for (int j = whole; j < steps; ++j) {
-    const uint8_t* kvs = sm.kv[j % 3];
-    fetch(j + 2);
-    // Values that are infinite or NaN, where some query may not see them.
-    if (threadIdx.x == 0) sm.wild = 0;
-    lds_barrier();
-    bool wild = false;
-    for (int c = (int)threadIdx.x; c < kKeys * VC; c += T)
-      wild |= abs_max_bits8(reinterpret_cast<const uint4*>(kvs + kKn + kKr)[c]) >= 0x7F80u;
-    if (wild) sm.wild = 1;
-    lds_barrier();
-#pragma unroll 1
-    for (int u = 0; u < 2; ++u) {
-      if (row0 + 31 + past < j * kKeys + 32 * u) break;        // no query of the wave sees a key
-      const int see = row + past - j * kKeys - 32 * u;         // this query sees the unit's keys 0 .. see
+  // Units at the edge: some query of the wave does not see all their keys.
+  for (; i < units; ++i) {
+    if (row0 < nq_in && row0 + 31 + past >= 32 * i) {          // some query of the wave sees a key
+      const uint8_t* s_v = s_kv[(i >> 1) % 3] + kKn + kKr + (i & 1) * 32 * VC * 16;
+      const int see = row + past - 32 * i;         // this query sees the unit's keys 0 .. see
       auto hidden = [&](int r) { return 8 * (r >> 2) + 4 * g + (r & 3) > see; };
-      s = scores(lds_address(kvs), u);
+      s = scores(step_of(i), i & 1);
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] = hidden(r) ? -INFINITY : s[r];
       refer(highest(s));
-      const float base = mx == -INFINITY ? 0.0f : mx;
+      base = mx == -INFINITY ? 0.0f : mx;
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const float w = __builtin_amdgcn_exp2f(fmaf(s[r], scale, -base));
         s[r] = hidden(r) ? 0.0f : w;
         sum += s[r];
       }
-      if (sm.wild) add_seen_values<VT, VC>(kvs + kKn + kKr + u * 32 * VC * 16, s, o, see, g, n);
-      else add_values(lds_address(kvs), u, s);
+      bool wild = false;                           // some value is infinite or NaN
+      for (int c = lane; c < 32 * VC; c += 64) wild |= abs_max_bits8(reinterpret_cast<const uint4*>(s_v)[c]) >= 0x7F80u;
+      if (__ballot(wild)) add_seen_values<VT, VC>(s_v, s, o, see, g, n);
+      else add_values(step_of(i), i & 1, s);
     }
-    wait_loads();
-    __syncthreads();
+    meet(i);
   }
   if (!in) return;
   sum += __shfl_xor(sum, 32);
