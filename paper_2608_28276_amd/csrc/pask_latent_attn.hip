@@ -39,6 +39,14 @@ __device__ __forceinline__ f32x4_t mfma(uint4 a, uint4 b, f32x4_t c) {
 // Sequence b has ceil(n_hi / 32) + ceil(n_lo / 32) tiles, or one if it holds
 // nothing (its worker writes the empty result).  Worker w of W takes tiles
 // [w u, w u + u), u = ceil(total / W).
+__device__ __forceinline__ int uni(int x) { return __builtin_amdgcn_readfirstlane(x); }
+struct Counts {                                    // as loaded: not looked at before they are needed
+  int n_hi, n_lo;
+};
+__device__ __forceinline__ Counts counts_at(const LatentAttnArgs& a, int b) {
+  const int32_t* c = counters_of(a.cv, min(b, a.batch - 1), a.layer);
+  return Counts{c[kCntHi], c[kCntLo]};
+}
 struct Seq {
   int b, n_hi, n_lo, nt_hi, nt;
   // Slots of tile j (0 or less: the tile of an empty sequence).
@@ -46,14 +54,16 @@ struct Seq {
     return j < nt_hi ? min(kTile, n_hi - j * kTile) : min(kTile, n_lo - (j - nt_hi) * kTile);
   }
 };
-__device__ __forceinline__ Seq seq_at(const LatentAttnArgs& a, int b) {
-  const int32_t* c = counters_of(a.cv, b, a.layer);
+__device__ __forceinline__ int tiles_of(int n_hi, int n_lo) {
+  return max(1, (n_hi + kTile - 1) / kTile + (n_lo + kTile - 1) / kTile);
+}
+__device__ __forceinline__ Seq seq_of(int b, const Counts& c) {
   Seq s;
   s.b = b;
-  s.n_hi = c[kCntHi];
-  s.n_lo = c[kCntLo];
+  s.n_hi = uni(c.n_hi);
+  s.n_lo = uni(c.n_lo);
   s.nt_hi = (s.n_hi + kTile - 1) / kTile;
-  s.nt = max(1, s.nt_hi + (s.n_lo + kTile - 1) / kTile);
+  s.nt = tiles_of(s.n_hi, s.n_lo);
   return s;
 }
 
@@ -68,9 +78,13 @@ template <int T, typename At>
 __device__ __forceinline__ ListPlace find_in_list(const LatentAttnArgs& a, long long* s_scan, At at) {
   constexpr int kWaves = T / 64;
   const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  auto tiles = [&](int b) {
+    const Counts c = counts_at(a, b);
+    return tiles_of(c.n_hi, c.n_lo);
+  };
   long long mine = 0;
   const int first = (int)((long long)a.batch * tid / T), last = (int)((long long)a.batch * (tid + 1) / T);
-  for (int b = first; b < last; ++b) mine += seq_at(a, b).nt;
+  for (int b = first; b < last; ++b) mine += tiles(b);
   long long incl = mine;
 #pragma unroll
   for (int off = 1; off < 64; off <<= 1) {
@@ -89,87 +103,114 @@ __device__ __forceinline__ ListPlace find_in_list(const LatentAttnArgs& a, long 
   if (x >= before && x < before + mine) {          // one thread at most
     int b = first;
     long long start = before;
-    for (int nt; start + (nt = seq_at(a, b).nt) <= x; ++b) start += nt;
+    for (int nt; start + (nt = tiles(b)) <= x; ++b) start += nt;
     s_scan[kWaves] = start;
     s_scan[kWaves + 1] = b;
   }
   __syncthreads();
-  return ListPlace{total, s_scan[kWaves], (int)s_scan[kWaves + 1]};
+  return ListPlace{total, s_scan[kWaves], uni((int)s_scan[kWaves + 1])};
+}
+
+// Tiles each worker takes.  More workers finish their tiles sooner but leave
+// more partial results, whose writing and merging costs about 1/40 of a tile's
+// time for 16 heads when the whole chip shares it: W tiles / u + W NHT / 40 is
+// least at W = sqrt(40 tiles / NHT) tiles' times.
+__device__ __forceinline__ long long tiles_per_worker(long long total, int workers, int head_tiles) {
+  const int best = (int)sqrtf(76.0f * (float)total / (float)head_tiles) + 1;
+  const int n = min(workers, best);
+  return (total + n - 1) / n;
 }
 
 // ---------------------------------------------------------------------------
 // one tile into LDS
 // ---------------------------------------------------------------------------
-// A HIGH tile is the two pages as they lie, copied without passing through
-// registers.  A LOW tile's codes, scales and rotary keys pass through registers
-// (loaded while the tile before is attended) and are widened on their way.
+// Pages are copied as they lie, without passing through registers.  Those of a
+// LOW tile go to the end of the tile's buffer, from where the tile is widened
+// in place once they have arrived (widen_low).
 template <int R, int P, int T>
 struct Tile {
   using PG = LatentPage<R, P>;
-  static constexpr int NC = (2 * PG::kGroups + T - 1) / T;     // code groups per thread of two LOW pages
-  uint4 codes[NC], rope;
-  uint16_t scale[NC];
+  static constexpr int kWaves = T / 64;
+  static constexpr int kBytes = 2 * PG::kHiBytes, kRaw = kBytes - 2 * PG::kLoBytes;
+  static constexpr int kLoChunks = PG::kLoBytes / 16;
 
-  // p0, p1: the two pages (p1 negative: none).  kWaves waves share the 1 KiB pieces.
+  // p0, p1: the two pages (p1 negative: none).  The waves share the 1 KiB pieces.
   __device__ __forceinline__ static void copy_high(const uint8_t* pool, int p0, int p1, uint8_t* tile, int wave,
                                                    int lane) {
-    const uint8_t* b0 = pool + (size_t)p0 * PG::kHiBytes;
-    const uint8_t* b1 = pool + (size_t)p1 * PG::kHiBytes - PG::kHiBytes;
-    const int n = p1 < 0 ? PG::KI : 2 * PG::KI;
+    const uint8_t* b0 = pool + (size_t)p0 * PG::kHiBytes + lane * 16;
+    if (p1 >= 0) {
+      const uint8_t* b1 = pool + (size_t)p1 * PG::kHiBytes - PG::kHiBytes + lane * 16;
 #pragma unroll
-    for (int k = 0; k < (2 * PG::KI + T / 64 - 1) / (T / 64); ++k) {
-      const int x = wave + k * (T / 64);
-      if (x < n) load_to_lds<true>((x < PG::KI ? b0 : b1) + x * 1024 + lane * 16, tile + x * 1024);
+      for (int k = 0; k < (2 * PG::KI + kWaves - 1) / kWaves; ++k) {
+        const int x = wave + k * kWaves;
+        if ((k + 1) * kWaves <= 2 * PG::KI || x < 2 * PG::KI)
+          load_to_lds<true>((x < PG::KI ? b0 : b1) + x * 1024, tile + x * 1024);
+      }
+    } else {
+      for (int x = wave; x < PG::KI; x += kWaves) load_to_lds<true>(b0 + x * 1024, tile + x * 1024);
+    }
+  }
+  __device__ __forceinline__ static void copy_low(const uint8_t* pool, int p0, int p1, uint8_t* tile, int wave, int lane) {
+    const uint8_t* b0 = pool + (size_t)p0 * PG::kLoBytes;
+    const uint8_t* b1 = pool + (size_t)(p1 < 0 ? p0 : p1) * PG::kLoBytes - PG::kLoBytes;
+#pragma unroll
+    for (int k = 0; k < (2 * kLoChunks + T - 1) / T; ++k) {
+      const int c = (wave + k * kWaves) * 64 + lane;
+      if (c < 2 * kLoChunks)
+        load_to_lds<true>((c < kLoChunks ? b0 : b1) + c * 16, tile + kRaw + (wave + k * kWaves) * 1024);
     }
   }
   // Slots from n on as zeros: what lies there is not an entry (any bytes, NaN
   // among them), and a weight of 0 does not make a NaN value harmless.
-  __device__ __forceinline__ static void clear_from(uint8_t* tile, int n) {
+  __device__ __forceinline__ static void clear_from(uint8_t* tile_buf, int n) {
+    const uint32_t tile = lds_address(tile_buf);
     for (int c = (int)threadIdx.x; c < 2 * PG::kHiChunks; c += T) {
       const int page = c < PG::kHiChunks ? 0 : 1, d = c - page * PG::kHiChunks;
       if (page * kPage + latent_swap((d >> 4) & 3, d & 15) >= n)
-        reinterpret_cast<uint4*>(tile)[c] = make_uint4(0u, 0u, 0u, 0u);
+        write_lds16(tile + c * 16, make_uint4(0u, 0u, 0u, 0u));
     }
   }
-  __device__ __forceinline__ void load_low(const uint8_t* pool, int p0, int p1) {
-    const uint8_t* b0 = pool + (size_t)p0 * PG::kLoBytes;
-    const uint8_t* b1 = pool + (size_t)(p1 < 0 ? p0 : p1) * PG::kLoBytes;
+  // The tile of n slots from the pages' bytes at its end, by the whole
+  // workgroup: all of them are read before the first value is written.
+  __device__ __forceinline__ static void widen_low(uint8_t* tile_buf, int n) {
+    const uint32_t tile = lds_address(tile_buf), raw = tile + kRaw;
+    constexpr int NC = (2 * PG::kGroups + T - 1) / T;          // code groups per thread
+    static_assert(2 * PG::kRopeChunks <= T, "a rotary piece per thread");
+    uint4 codes[NC], rope = make_uint4(0u, 0u, 0u, 0u);
+    float scale[NC];
 #pragma unroll
     for (int k = 0; k < NC; ++k) {
-      const int g = (int)threadIdx.x + T * k, h = g < PG::kGroups ? g : g - PG::kGroups;
-      const uint8_t* pg = g < PG::kGroups ? b0 : b1;
+      const int g = (int)threadIdx.x + T * k, page = g < PG::kGroups ? 0 : 1, h = g - page * PG::kGroups;
       if (g < 2 * PG::kGroups) {
-        codes[k] = stream_load16(pg + h * 16);
-        scale[k] = *reinterpret_cast<const uint16_t*>(pg + PG::kScales + 2 * h);
+        codes[k] = read_lds16(raw + page * PG::kLoBytes + h * 16);
+        scale[k] = half_value(
+            *reinterpret_cast<const uint16_t*>(tile_buf + kRaw + page * PG::kLoBytes + PG::kScales + 2 * h));
       }
     }
-    const int c = (int)threadIdx.x, d = c < PG::kRopeChunks ? c : c - PG::kRopeChunks;
-    static_assert(2 * PG::kRopeChunks <= T, "a rotary piece per thread");
-    if (c < 2 * PG::kRopeChunks) rope = stream_load16((c < PG::kRopeChunks ? b0 : b1) + PG::kRopeAt + d * 16);
-  }
-  __device__ __forceinline__ void store_low(uint8_t* tile, int n) const {
+    const int c = (int)threadIdx.x, rp = c < PG::kRopeChunks ? 0 : 1, rd = c - rp * PG::kRopeChunks;
+    if (c < 2 * PG::kRopeChunks)
+      rope = read_lds16(raw + rp * PG::kLoBytes + PG::kRopeAt + rd * 16);
+    lds_barrier();
 #pragma unroll
     for (int k = 0; k < NC; ++k) {
       const int g = (int)threadIdx.x + T * k, page = g < PG::kGroups ? 0 : 1, h = g - page * PG::kGroups;
       if (g < 2 * PG::kGroups) {
         const int t = h & 15;
         const bool in = page * kPage + t < n;
-        const float s = half_value(scale[k]);
         const uint32_t w[4] = {codes[k].x, codes[k].y, codes[k].z, codes[k].w};
-        uint8_t* dst = tile + page * PG::kHiBytes + (h >> 4) * 1024;
+        const uint32_t dst = tile + page * PG::kHiBytes + (h >> 4) * 1024;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const uint4 v = low_values(w[q], s);
-          *reinterpret_cast<uint4*>(dst + (16 * q + latent_swap(q, t)) * 16) = in ? v : make_uint4(0u, 0u, 0u, 0u);
+          const uint4 v = low_values(w[q], scale[k]);
+          write_lds16(dst + (16 * q + latent_swap(q, t)) * 16, in ? v : make_uint4(0u, 0u, 0u, 0u));
         }
       }
     }
-    const int c = (int)threadIdx.x, page = c < PG::kRopeChunks ? 0 : 1, d = c - page * PG::kRopeChunks;
     if (c < 2 * PG::kRopeChunks) {
-      const int slot = page * kPage + latent_swap((d >> 4) & 3, d & 15);
-      *reinterpret_cast<uint4*>(tile + page * PG::kHiBytes + PG::RI * 1024 + d * 16) =
-          slot < n ? rope : make_uint4(0u, 0u, 0u, 0u);
+      const int slot = rp * kPage + latent_swap((rd >> 4) & 3, rd & 15);
+      write_lds16(tile + rp * PG::kHiBytes + PG::RI * 1024 + rd * 16, slot < n ? rope : make_uint4(0u, 0u, 0u, 0u));
     }
+    lds_barrier();
   }
 };
 
@@ -177,68 +218,103 @@ struct Tile {
 // attention
 // ---------------------------------------------------------------------------
 // Per tile (32 slots, all heads; NHT tiles of 16 heads):
-//   scores  S^T = C Q^T on v_mfma_f32_16x16x32_bf16, a wave per head tile:
-//           lane (q, n) holds head n's scores of slots 4q .. 4q + 3 of both
-//           pages; queries stay in registers.
-//   weights online softmax in base 2; the reference m of a head moves only
-//           when a tile's maximum exceeds it by more than 8, so weights stay
-//           below 2^8 and the sums are rarely rescaled.  Weights are rounded
-//           to bf16 (half a step, 2^-8 of a weight; independent over slots, so
-//           it averages out below the output's own rounding); their sum is
-//           kept of the unrounded ones in fp32.
+//   scores  S^T = C Q^T on v_mfma_f32_16x16x32_bf16, a wave per head tile (per
+//           page of a head tile, up to 32 heads): lane (q, n) holds head n's
+//           scores of slots 4q .. 4q + 3 of a page; queries stay in registers.
+//   weights online softmax in base 2.  Weights are rounded to bf16 (half a step,
+//           2^-8 of a weight; independent over slots, so it averages out below
+//           the output's own rounding); their sum is kept of the unrounded ones
+//           in fp32.  A head's reference moves only when a score exceeds it by
+//           more than kHeadroom: weights up to 2^60 are as precise as those
+//           below 1, and the sums of values, which fill the registers, are left
+//           alone in the loop.
 //   values  O^T += C^T P^T: wave w of W owns output elements [w R / W, (w + 1) R
 //           / W) of every head, so a value is read from LDS once per workgroup;
 //           weights pass through LDS in the operand order (a score lane holds
-//           exactly one operand lane's 8 weights).
-// The next tile, also across sequences, is on its way into the other LDS
-// buffer meanwhile.
+//           exactly one operand lane's weights).
+// The next tile, also across sequences, is on its way into the other LDS buffer
+// meanwhile, and the page ids of the one after it into registers.
 constexpr int latent_waves(int head_tiles) { return head_tiles >= 8 ? 8 : 4; }
+constexpr float kHeadroom = 60.0f;
 
 template <int R, int P, int NHT>
 __global__ __launch_bounds__(64 * latent_waves(NHT), 2) void latent_attn_kernel(LatentAttnArgs a) {
   using PG = LatentPage<R, P>;
   constexpr int NW = latent_waves(NHT), T = 64 * NW;
   constexpr int KI = PG::KI, DT = R / (16 * NW);   // score steps; 16-element output tiles of a wave
+  constexpr int JP = NHT <= 2 ? 1 : 2;             // pages per scoring wave
+  constexpr int QW = NHT * 2 / JP;                 // scoring waves
+  static_assert(QW <= NW, "a wave per score job");
   __shared__ __align__(16) struct {
     uint8_t tile[2][2 * PG::kHiBytes];
-    uint4 p[NHT * 64];
+    uint8_t p[NHT * 1024];
     long long scan[NW + 2];
-    float alpha[NHT * 16];
-    int grown[NHT];
+    float top[QW * 16], sum[QW * 16], alpha[NHT * 16];
+    int grown[QW];
   } sm;
   const CacheView& cv = a.cv;
-  const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int lane = (int)threadIdx.x & 63, wave = uni((int)threadIdx.x >> 6);
   const int q4 = lane >> 4, n = lane & 15;
+  const int ht = JP == 1 ? wave >> 1 : wave, page0 = JP == 1 ? wave & 1 : 0;   // a scoring wave's job
+  const bool scores = wave < QW;
   long long units = 1;
   const ListPlace place = find_in_list<T>(a, sm.scan, [&](long long total) {
-    units = (total + a.workers - 1) / a.workers;
+    units = tiles_per_worker(total, a.workers, NHT);
     return (long long)blockIdx.x * units;
   });
   const long long u0 = (long long)blockIdx.x * units, u1 = u0 + units < place.total ? u0 + units : place.total;
   if (u0 >= place.total) return;
   const int e = (n & 3) >> 1;                      // value operand: quarter, slot and half of a lane's 8 bytes
   const int v_at = (e * 16 + ((4 * q4 + (n >> 2)) ^ (8 * e))) * 16 + 8 * (n & 1) + wave * DT * 512;
-  const int k_at = (16 * q4 + latent_swap(q4, n)) * 16;
-  Tile<R, P, T> low;
-  auto fetch = [&](const Seq& s, int j, uint8_t* tile) {
-    const int m = s.slots(j);
-    if (m <= 0) return;
-    const bool high = j < s.nt_hi;
-    const int32_t* bt = block_table_of(cv, s.b, a.layer, high ? kHi : kLo) + 2 * (high ? j : j - s.nt_hi);
-    const int p0 = bt[0], p1 = m > kPage ? bt[1] : -1;
-    if (high) Tile<R, P, T>::copy_high(cv.hi_pool, p0, p1, tile, wave, lane);
-    else low.load_low(cv.lo_pool, p0, p1);
+  const int k_at = (16 * q4 + latent_swap(q4, n)) * 16 + page0 * PG::kHiBytes;
+
+  // The walk over the list: the current tile, the next (its page ids known) and
+  // the one after it (its page ids under way), and the counts of the sequence
+  // behind that one.
+  struct Place {
+    Seq s;
+    int j;
+  };
+  struct Pages {
+    int p0, p1;
+  };
+  Counts ahead;
+  auto pages_of = [&](const Place& x) {
+    Pages g{0, -1};
+    const int m = x.s.slots(x.j);
+    if (m > 0) {
+      const bool high = x.j < x.s.nt_hi;
+      const int32_t* bt = block_table_of(cv, x.s.b, a.layer, high ? kHi : kLo) + 2 * (high ? x.j : x.j - x.s.nt_hi);
+      g.p0 = bt[0];
+      if (m > kPage) g.p1 = bt[1];
+    }
+    return g;
+  };
+  auto after = [&](const Place& x) {
+    Place y = x;
+    if (++y.j == y.s.nt) {
+      y.s = seq_of(x.s.b + 1, ahead);
+      y.j = 0;
+      ahead = counts_at(a, y.s.b + 1);
+    }
+    return y;
+  };
+  using TL = Tile<R, P, T>;
+  auto fetch = [&](const Place& x, const Pages& g, uint8_t* tile) {
+    if (x.s.slots(x.j) <= 0) return;
+    if (x.j < x.s.nt_hi) TL::copy_high(cv.hi_pool, uni(g.p0), uni(g.p1), tile, wave, lane);
+    else TL::copy_low(cv.lo_pool, uni(g.p0), uni(g.p1), tile, wave, lane);
   };
   uint4 qf[KI];
   auto load_queries = [&](int b) {
-    const int head = wave * 16 + n;
+    const int head = ht * 16 + n;
     const uint16_t* src = a.q + ((size_t)b * a.heads + head) * (R + P) + 8 * q4;
 #pragma unroll
     for (int i = 0; i < KI; ++i)
-      qf[i] = wave < NHT && head < a.heads ? *reinterpret_cast<const uint4*>(src + 32 * i) : make_uint4(0u, 0u, 0u, 0u);
+      qf[i] = scores && head < a.heads ? *reinterpret_cast<const uint4*>(src + 32 * i) : make_uint4(0u, 0u, 0u, 0u);
   };
   f32x4_t acc[NHT][DT];
-  float mx = -INFINITY, sum = 0.0f;
+  float x[4 * JP], mx, sum, part = 0.0f, top = -INFINITY;      // scaled scores of the tile, reference, sums
   auto restart = [&]() {
 #pragma unroll
     for (int h = 0; h < NHT; ++h)
@@ -247,181 +323,264 @@ __global__ __launch_bounds__(64 * latent_waves(NHT), 2) void latent_attn_kernel(
     mx = -INFINITY;
     sum = 0.0f;
   };
-  restart();
-
-  Seq s = seq_at(a, place.b);
-  long long start = place.start;                   // the list's tile 0 of sequence s
-  int j = (int)(u0 - start), buf = 0;
-  load_queries(s.b);
-  fetch(s, j, sm.tile[0]);
-  if (j >= s.nt_hi && s.slots(j) > 0) low.store_low(sm.tile[0], s.slots(j));
-  wait_loads();
-  __syncthreads();
-  for (long long u = u0; u < u1; ++u) {
-    uint8_t* tile = sm.tile[buf];
-    uint8_t* other = sm.tile[buf ^ 1];
-    const int m = s.slots(j);
-    const bool ends = j + 1 == s.nt || u + 1 == u1;             // the worker's last tile of this sequence
-    Seq next = s;
-    int nj = j + 1;
-    if (j + 1 == s.nt && u + 1 < u1) {
-      next = seq_at(a, s.b + 1);
-      nj = 0;
+  auto weigh = [&]() {                             // weights of x into LDS
+    const float base = mx == -INFINITY ? 0.0f : mx;
+    float w[4 * JP];
+    part = 0.0f;
+#pragma unroll
+    for (int r = 0; r < 4 * JP; ++r) {
+      w[r] = __builtin_amdgcn_exp2f(x[r] - base);
+      part += w[r];
     }
-    if (u + 1 < u1) fetch(next, nj, other);
-    if (m < kTile && (j < s.nt_hi || m <= 0)) {    // a HIGH store's last tile, or an empty sequence's
-      Tile<R, P, T>::clear_from(tile, m);
+#pragma unroll
+    for (int jp = 0; jp < JP; ++jp)
+      write_lds8(lds_address(sm.p) + (ht * 64 + lane) * 16 + (page0 + jp) * 8,
+                 make_uint2(pack_bf16x2(w[4 * jp], w[4 * jp + 1]), pack_bf16x2(w[4 * jp + 2], w[4 * jp + 3])));
+  };
+  // Scores and weights of a tile in LDS; true for every wave if some head's
+  // reference has to move first (move_reference).
+  auto score = [&](const Place& at, uint8_t* tile) {
+    const int m = at.s.slots(at.j);
+    if (at.j >= at.s.nt_hi && m > 0) {
+      TL::widen_low(tile, m);
+    } else if (m < kTile) {                        // a HIGH store's last tile, or an empty sequence's
+      TL::clear_from(tile, m);
       lds_barrier();
     }
-    if (wave < NHT) {
-      f32x4_t s0 = {0.0f, 0.0f, 0.0f, 0.0f}, s1 = s0;
+    if (scores) {
+      f32x4_t s[JP];
 #pragma unroll
-      for (int i = 0; i < KI; ++i) {
-        s0 = mfma(*reinterpret_cast<const uint4*>(tile + i * 1024 + k_at), qf[i], s0);
-        s1 = mfma(*reinterpret_cast<const uint4*>(tile + PG::kHiBytes + i * 1024 + k_at), qf[i], s1);
-      }
-      float x[8], top = -INFINITY;
+      for (int jp = 0; jp < JP; ++jp) s[jp] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int r = 0; r < 8; ++r) {
-        const int slot = (r < 4 ? 0 : kPage) + 4 * q4 + (r & 3);
-        x[r] = slot < m ? (r < 4 ? s0[r & 3] : s1[r & 3]) * a.scale_log2 : -INFINITY;
+      for (int i = 0; i < KI; ++i)
+#pragma unroll
+        for (int jp = 0; jp < JP; ++jp)
+          s[jp] = mfma(read_lds16(lds_address(tile) + jp * PG::kHiBytes + i * 1024 + k_at), qf[i], s[jp]);
+      top = -INFINITY;
+#pragma unroll
+      for (int r = 0; r < 4 * JP; ++r) {
+        const int slot = (page0 + (r >> 2)) * kPage + 4 * q4 + (r & 3);
+        x[r] = slot < m ? s[r >> 2][r & 3] * a.scale_log2 : -INFINITY;
         top = fmaxf(top, x[r]);
       }
-      top = fmaxf(top, __shfl_xor(top, 16));
-      top = fmaxf(top, __shfl_xor(top, 32));
-      const float ref = top > mx + 8.0f ? top : mx;
-      const float alpha = ref == mx ? 1.0f : __builtin_amdgcn_exp2f(mx - ref);
-      mx = ref;
-      const float base = ref == -INFINITY ? 0.0f : ref;
-      float part = 0.0f;
-#pragma unroll
-      for (int r = 0; r < 8; ++r) {
-        x[r] = __builtin_amdgcn_exp2f(x[r] - base);
-        part += x[r];
-      }
-      sum = sum * alpha + part;
-      sm.p[wave * 64 + lane] = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
-                                         pack_bf16x2(x[6], x[7]));
-      if (q4 == 0) sm.alpha[wave * 16 + n] = alpha;
-      const bool grown = __ballot(alpha != 1.0f) != 0ull;
+      weigh();
+      const bool grown = __ballot(top > mx + kHeadroom) != 0ull;
       if (lane == 0) sm.grown[wave] = grown;
     }
     lds_barrier();
     int grown = 0;
 #pragma unroll
-    for (int h = 0; h < NHT; ++h) grown |= sm.grown[h];
-    if (__builtin_amdgcn_readfirstlane(grown)) {
-#pragma unroll
-      for (int h = 0; h < NHT; ++h) {
-        const float alpha = sm.alpha[h * 16 + n];
-#pragma unroll
-        for (int d = 0; d < DT; ++d) acc[h][d] *= alpha;
-      }
+    for (int w = 0; w < QW; ++w) grown |= sm.grown[w];
+    return uni(grown) != 0;
+  };
+  auto move_reference = [&]() {
+    if (scores) {
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      if (q4 == 0) sm.top[wave * 16 + n] = top;
     }
-    uint4 pf[NHT];
+    lds_barrier();
+    if (scores) {
+      if constexpr (JP == 1) top = fmaxf(top, sm.top[(wave ^ 1) * 16 + n]);
+      const float ref = top > mx + kHeadroom ? top : mx;
+      const float alpha = ref == mx ? 1.0f : __builtin_amdgcn_exp2f(mx - ref);
+      mx = ref;
+      sum *= alpha;
+      weigh();
+      if (q4 == 0 && page0 == 0) sm.alpha[ht * 16 + n] = alpha;
+    }
+    lds_barrier();
 #pragma unroll
-    for (int h = 0; h < NHT; ++h) pf[h] = sm.p[h * 64 + lane];
+    for (int h = 0; h < NHT; ++h) {
+      const float alpha = sm.alpha[h * 16 + n];
+#pragma unroll
+      for (int d = 0; d < DT; ++d) acc[h][d] *= alpha;
+    }
+  };
+  auto add_values = [&](const uint8_t* tile) {
     const uint32_t vs = lds_address(tile) + v_at;
-    auto add_values = [&](auto first) {            // output tiles first .. + 3 (those below DT)
+    auto four = [&](auto first) {                  // output tiles first .. + 3 (those below DT)
       constexpr int d0 = decltype(first)::value, k = d0 * 512;
       constexpr int k1 = DT > d0 + 1 ? k + 512 : k, k2 = DT > d0 + 2 ? k + 1024 : k, k3 = DT > d0 + 3 ? k + 1536 : k;
       uint4 v[4];
       read_transposed<k, k1, k2, k3, PG::kHiBytes>(vs, vs, vs, vs, v);
 #pragma unroll
-      for (int d = 0; d < 4; ++d)
-#pragma unroll
-        for (int h = 0; h < NHT; ++h)
-          if (d0 + d < DT) acc[h][d0 + d] = mfma(v[d], pf[h], acc[h][d0 + d]);
-    };
-    add_values(std::integral_constant<int, 0>{});
-    if constexpr (DT > 4) add_values(std::integral_constant<int, 4>{});
-    if (u + 1 < u1 && nj >= next.nt_hi && next.slots(nj) > 0) low.store_low(other, next.slots(nj));
-
-    if (ends) {
-      // Results: the whole history, or a part of it in slot 2w (the worker's
-      // first sequence) or 2w + 1 of the partials.
-      const bool whole = start >= u0 && start + s.nt <= u1;
-      const int part = 2 * (int)blockIdx.x + (start > u0 ? 1 : 0);
-      if (threadIdx.x == 0 && start >= u0) {
-        a.ws_seq[2 * s.b] = part;
-        a.ws_seq[2 * s.b + 1] = whole ? 0 : (int)((start + s.nt - 1) / units) - (int)blockIdx.x + 1;
-      }
-      lds_barrier();                               // the scale factors have been read
-      if (wave < NHT) {
-        sum += __shfl_xor(sum, 16);
-        sum += __shfl_xor(sum, 32);
-        const int head = wave * 16 + n;
-        if (q4 == 0) {
-          sm.alpha[head] = sum == 0.0f ? 0.0f : 1.0f / sum;
-          if (whole) {
-            if (a.lse && head < a.heads)
-              a.lse[(size_t)s.b * a.heads + head] =
-                  sum == 0.0f ? -INFINITY : (mx + __builtin_amdgcn_logf(sum)) * kLn2;
-          } else {
-            float* ml = a.ws_ml + ((size_t)part * NHT * 16 + head) * 2;
-            ml[0] = mx;
-            ml[1] = sum;
-          }
-        }
-      }
-      if (u + 1 < u1) load_queries(next.b);
-      lds_barrier();
-#pragma unroll
       for (int h = 0; h < NHT; ++h) {
-        const int head = h * 16 + n;
-        if (head < a.heads) {
-          const float inv = sm.alpha[head];
+        const uint4 w = read_lds16(lds_address(sm.p) + (h * 64 + lane) * 16);
 #pragma unroll
-          for (int d = 0; d < DT; ++d) {
-            const int dim = 16 * (wave * DT + d) + 4 * q4;
-            const f32x4_t o = acc[h][d];
-            if (whole) {
-              *reinterpret_cast<uint2*>(a.out + ((size_t)s.b * a.heads + head) * R + dim) =
-                  make_uint2(pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv));
-            } else {
-              *reinterpret_cast<f32x4_t*>(a.ws_o + ((size_t)part * NHT * 16 + head) * R + dim) = o;
-            }
-          }
-        }
+        for (int d = 0; d < 4; ++d)
+          if (d0 + d < DT) acc[h][d0 + d] = mfma(v[d], w, acc[h][d0 + d]);
       }
-      restart();
-      if (nj == 0) start += s.nt;
+    };
+    four(std::integral_constant<int, 0>{});
+    if constexpr (DT > 4) four(std::integral_constant<int, 4>{});
+  };
+
+  Place cur, next, later;
+  Pages next_pages, later_pages;
+  ahead = counts_at(a, place.b + 1);
+  cur.s = seq_of(place.b, counts_at(a, place.b));
+  cur.j = (int)(u0 - place.start);
+  long long start = place.start, u = u0;           // the list's tile 0 of cur.s; cur's place in the list
+  const Pages first = pages_of(cur);
+  next = cur;
+  next_pages = first;
+  if (u + 1 < u1) {
+    next = after(cur);
+    next_pages = pages_of(next);
+  }
+  later = next;
+  later_pages = next_pages;
+  int buf = 0;
+  load_queries(cur.s.b);
+  restart();
+  fetch(cur, first, sm.tile[0]);
+  wait_loads();
+  __syncthreads();
+  // Everything of the tile before is done with: the next tile on its way into
+  // the free buffer, the page ids of the one after it.
+  auto look_ahead = [&]() {
+    if (u + 1 < u1) fetch(next, next_pages, sm.tile[buf ^ 1]);
+    if (u + 2 < u1) {
+      later = after(next);
+      later_pages = pages_of(later);
     }
-    s = next;
-    j = nj;
+  };
+  auto advance = [&]() {
+    cur = next;
+    next = later;
+    next_pages = later_pages;
+    ++u;
     buf ^= 1;
     wait_loads();
     __syncthreads();
+  };
+  look_ahead();
+  bool grown = score(cur, sm.tile[buf]);
+  for (;;) {
+    if (grown) move_reference();
+    bool ends;
+    for (;;) {                                     // tiles of one sequence, until a reference has to move
+      sum += part;
+      add_values(sm.tile[buf]);
+      ends = cur.j + 1 == cur.s.nt || u + 1 == u1;             // the worker's last tile of this sequence
+      if (ends) break;
+      advance();
+      look_ahead();
+      grown = score(cur, sm.tile[buf]);
+      if (grown) break;
+    }
+    if (!ends) continue;
+
+    // Results: the whole history, or a part of it in slot 2w (the worker's
+    // first sequence) or 2w + 1 of the partials.
+    const Seq s = cur.s;
+    const bool whole = start >= u0 && start + s.nt <= u1;
+    const int slot = 2 * (int)blockIdx.x + (start > u0 ? 1 : 0);
+    if (threadIdx.x == 0 && start >= u0) {
+      a.ws_seq[2 * s.b] = slot;
+      a.ws_seq[2 * s.b + 1] = whole ? 0 : (int)((start + s.nt - 1) / units) - (int)blockIdx.x + 1;
+    }
+    if (scores) {
+      sum += __shfl_xor(sum, 16);
+      sum += __shfl_xor(sum, 32);
+      if (q4 == 0) sm.sum[wave * 16 + n] = sum;
+    }
+    lds_barrier();
+    if (scores && page0 == 0 && q4 == 0) {
+      if constexpr (JP == 1) sum += sm.sum[(wave + 1) * 16 + n];
+      const int head = ht * 16 + n;
+      sm.alpha[head] = sum == 0.0f ? 0.0f : 1.0f / sum;
+      if (whole) {
+        if (a.lse && head < a.heads)
+          a.lse[(size_t)s.b * a.heads + head] = sum == 0.0f ? -INFINITY : (mx + __builtin_amdgcn_logf(sum)) * kLn2;
+      } else {
+        float* ml = a.ws_ml + ((size_t)slot * NHT * 16 + head) * 2;
+        ml[0] = mx;
+        ml[1] = sum;
+      }
+    }
+    const bool more = u + 1 < u1;
+    if (more) load_queries(next.s.b);
+    lds_barrier();
+#pragma unroll
+    for (int h = 0; h < NHT; ++h) {
+      const int head = h * 16 + n;
+      if (head < a.heads) {
+        const float inv = sm.alpha[head];
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          const int dim = 16 * (wave * DT + d) + 4 * q4;
+          const f32x4_t o = acc[h][d];
+          if (whole) {
+            *reinterpret_cast<uint2*>(a.out + ((size_t)s.b * a.heads + head) * R + dim) =
+                make_uint2(pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv));
+          } else {
+            *reinterpret_cast<f32x4_t*>(a.ws_o + ((size_t)slot * NHT * 16 + head) * R + dim) = o;
+          }
+        }
+      }
+    }
+    if (!more) return;
+    start += s.nt;
+    restart();
+    advance();
+    look_ahead();
+    grown = score(cur, sm.tile[buf]);
   }
 }
 
 // ---------------------------------------------------------------------------
 // merge
 // ---------------------------------------------------------------------------
-// A wave per head: the partials' maxima and sums give each one's weight, then
-// the sums of values are added in order of the partials (slot of the first,
-// then the first slots of the workers after it).
+// The partials of a head: maxima and sums give each one's weight, then the
+// weighted values are added in order of the partials (slot of the first, then
+// the first slots of the workers after it).  Few partials: a wave per head.
+// Many: a workgroup per head, its waves taking every fourth partial and adding
+// up through LDS.
 template <int R>
 __global__ __launch_bounds__(kThreads) void latent_merge_kernel(LatentAttnArgs a, int tile_heads) {
+  constexpr int E = R / 64;                        // elements per lane
+  __shared__ float s_o[kWaves][R], s_w[kWaves];
   const int b = blockIdx.y, lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
   const int first = a.ws_seq[2 * b], n = a.ws_seq[2 * b + 1];
   if (n == 0) return;
-  constexpr int E = R / 64;                        // elements per lane
+  const bool shared = n > 8;                       // by all waves of the workgroup
   auto slot = [&](int k) { return k == 0 ? first : 2 * (first / 2 + k); };
-  for (int h = (int)blockIdx.x * kWaves + wave; h < a.heads; h += (int)gridDim.x * kWaves) {
+  const int step = shared ? (int)gridDim.x : (int)gridDim.x * kWaves;
+  for (int h0 = shared ? (int)blockIdx.x : (int)blockIdx.x * kWaves; h0 < a.heads; h0 += step) {
+    const int h = shared ? h0 : h0 + wave;
+    if (h >= a.heads) continue;                    // only of a wave with a head of its own
     float top = -INFINITY;
     for (int k = lane; k < n; k += 64) top = fmaxf(top, a.ws_ml[((size_t)slot(k) * tile_heads + h) * 2]);
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
     const float base = top == -INFINITY ? 0.0f : top;
     float o[E] = {}, total = 0.0f;
-    for (int k = 0; k < n; ++k) {
+    const int k0 = shared ? wave : 0, dk = shared ? kWaves : 1;
+#pragma unroll 4
+    for (int k = k0; k < n; k += dk) {
       const size_t at = (size_t)slot(k) * tile_heads + h;
-      const float w = __builtin_amdgcn_exp2f(a.ws_ml[at * 2] - base);
-      total += w * a.ws_ml[at * 2 + 1];
+      const float2 ml = *reinterpret_cast<const float2*>(a.ws_ml + at * 2);
       const float* src = a.ws_o + at * R + lane * E;
+      const float w = __builtin_amdgcn_exp2f(ml.x - base);
+      total += w * ml.y;
 #pragma unroll
       for (int u = 0; u < E; ++u) o[u] += w * src[u];
+    }
+    if (shared) {
+      __syncthreads();                             // the head before has been read
+#pragma unroll
+      for (int u = 0; u < E; ++u) s_o[wave][lane * E + u] = o[u];
+      if (lane == 0) s_w[wave] = total;
+      __syncthreads();
+      if (wave > 0) continue;
+#pragma unroll
+      for (int w = 1; w < kWaves; ++w) {
+        total += s_w[w];
+#pragma unroll
+        for (int u = 0; u < E; ++u) o[u] += s_o[w][lane * E + u];
+      }
     }
     const float inv = total == 0.0f ? 0.0f : 1.0f / total;
     const size_t at = (size_t)b * a.heads + h;
@@ -466,7 +625,7 @@ hipError_t launch_latent_attention(const LatentAttnArgs& a, hipStream_t s) {
   if (e != hipSuccess) return e;
   if (a.workers == 1) return hipSuccess;           // nothing is shared
   const int heads = 16 * latent_head_tiles(a.heads);
-  const dim3 grid(std::max(1, std::min((a.heads + kWaves - 1) / kWaves, 1024 / a.batch)), a.batch);
+  const dim3 grid(std::max(1, std::min(a.heads, 1024 / a.batch)), a.batch);
   if (a.rank == 128) latent_merge_kernel<128><<<grid, dim3(kThreads), 0, s>>>(a, heads);
   else if (a.rank == 256) latent_merge_kernel<256><<<grid, dim3(kThreads), 0, s>>>(a, heads);
   else latent_merge_kernel<512><<<grid, dim3(kThreads), 0, s>>>(a, heads);

@@ -80,10 +80,19 @@ __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
+// 16 and 8 bytes of LDS by address, as plain vectors: before accesses of the
+// struct types uint4 and uint2 the compiler waits for every copy under way.
+typedef __attribute__((address_space(3))) u32x4_t lds_u32x4;
+typedef __attribute__((address_space(3))) u32x2_t lds_u32x2;
 __device__ __forceinline__ uint4 read_lds16(uint32_t lds) {
-  typedef __attribute__((address_space(3))) u32x4_t lds_u32x4;
   const u32x4_t x = *(const lds_u32x4*)(uintptr_t)lds;
   return make_uint4(x[0], x[1], x[2], x[3]);
+}
+__device__ __forceinline__ void write_lds16(uint32_t lds, const uint4& v) {
+  *(lds_u32x4*)(uintptr_t)lds = u32x4_t{v.x, v.y, v.z, v.w};
+}
+__device__ __forceinline__ void write_lds8(uint32_t lds, const uint2& v) {
+  *(lds_u32x2*)(uintptr_t)lds = u32x2_t{v.x, v.y};
 }
 __device__ __forceinline__ uint32_t lds_address(const uint8_t* p) {
   return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint8_t*)p;
