@@ -49,10 +49,6 @@ __device__ __forceinline__ Counts counts_at(const LatentAttnArgs& a, int b) {
 }
 struct Seq {
   int b, n_hi, n_lo, nt_hi, nt;
-  // Slots of tile j (0 or less: the tile of an empty sequence).
-  __device__ __forceinline__ int slots(int j) const {
-    return j < nt_hi ? min(kTile, n_hi - j * kTile) : min(kTile, n_lo - (j - nt_hi) * kTile);
-  }
 };
 __device__ __forceinline__ int tiles_of(int n_hi, int n_lo) {
   return max(1, (n_hi + kTile - 1) / kTile + (n_lo + kTile - 1) / kTile);
@@ -137,6 +133,7 @@ struct Tile {
   // p0, p1: the two pages (p1 negative: none).  The waves share the 1 KiB pieces.
   __device__ __forceinline__ static void copy_high(const uint8_t* pool, int p0, int p1, uint8_t* tile, int wave,
                                                    int lane) {
+    lane = fresh(lane);
     const uint8_t* b0 = pool + (size_t)p0 * PG::kHiBytes + lane * 16;
     if (p1 >= 0) {
       const uint8_t* b1 = pool + (size_t)p1 * PG::kHiBytes - PG::kHiBytes + lane * 16;
@@ -151,6 +148,7 @@ struct Tile {
     }
   }
   __device__ __forceinline__ static void copy_low(const uint8_t* pool, int p0, int p1, uint8_t* tile, int wave, int lane) {
+    lane = fresh(lane);
     const uint8_t* b0 = pool + (size_t)p0 * PG::kLoBytes;
     const uint8_t* b1 = pool + (size_t)(p1 < 0 ? p0 : p1) * PG::kLoBytes - PG::kLoBytes;
 #pragma unroll
@@ -164,7 +162,7 @@ struct Tile {
   // among them), and a weight of 0 does not make a NaN value harmless.
   __device__ __forceinline__ static void clear_from(uint8_t* tile_buf, int n) {
     const uint32_t tile = lds_address(tile_buf);
-    for (int c = (int)threadIdx.x; c < 2 * PG::kHiChunks; c += T) {
+    for (int c = fresh((int)threadIdx.x); c < 2 * PG::kHiChunks; c += T) {
       const int page = c < PG::kHiChunks ? 0 : 1, d = c - page * PG::kHiChunks;
       if (page * kPage + latent_swap((d >> 4) & 3, d & 15) >= n)
         write_lds16(tile + c * 16, make_uint4(0u, 0u, 0u, 0u));
@@ -174,26 +172,27 @@ struct Tile {
   // workgroup: all of them are read before the first value is written.
   __device__ __forceinline__ static void widen_low(uint8_t* tile_buf, int n) {
     const uint32_t tile = lds_address(tile_buf), raw = tile + kRaw;
+    const int tid = fresh((int)threadIdx.x);
     constexpr int NC = (2 * PG::kGroups + T - 1) / T;          // code groups per thread
     static_assert(2 * PG::kRopeChunks <= T, "a rotary piece per thread");
     uint4 codes[NC], rope = make_uint4(0u, 0u, 0u, 0u);
     float scale[NC];
 #pragma unroll
     for (int k = 0; k < NC; ++k) {
-      const int g = (int)threadIdx.x + T * k, page = g < PG::kGroups ? 0 : 1, h = g - page * PG::kGroups;
+      const int g = tid + T * k, page = g < PG::kGroups ? 0 : 1, h = g - page * PG::kGroups;
       if (g < 2 * PG::kGroups) {
         codes[k] = read_lds16(raw + page * PG::kLoBytes + h * 16);
         scale[k] = half_value(
             *reinterpret_cast<const uint16_t*>(tile_buf + kRaw + page * PG::kLoBytes + PG::kScales + 2 * h));
       }
     }
-    const int c = (int)threadIdx.x, rp = c < PG::kRopeChunks ? 0 : 1, rd = c - rp * PG::kRopeChunks;
+    const int c = tid, rp = c < PG::kRopeChunks ? 0 : 1, rd = c - rp * PG::kRopeChunks;
     if (c < 2 * PG::kRopeChunks)
       rope = read_lds16(raw + rp * PG::kLoBytes + PG::kRopeAt + rd * 16);
     lds_barrier();
 #pragma unroll
     for (int k = 0; k < NC; ++k) {
-      const int g = (int)threadIdx.x + T * k, page = g < PG::kGroups ? 0 : 1, h = g - page * PG::kGroups;
+      const int g = tid + T * k, page = g < PG::kGroups ? 0 : 1, h = g - page * PG::kGroups;
       if (g < 2 * PG::kGroups) {
         const int t = h & 15;
         const bool in = page * kPage + t < n;
@@ -232,9 +231,13 @@ struct Tile {
 //           / W) of every head, so a value is read from LDS once per workgroup;
 //           weights pass through LDS in the operand order (a score lane holds
 //           exactly one operand lane's weights).
-// The next tile, also across sequences, is on its way into the other LDS buffer
-// meanwhile, and the page ids of the one after it into registers.
-constexpr int latent_waves(int head_tiles) { return head_tiles >= 8 ? 8 : 4; }
+// The next tiles, also across sequences, are on their way into the other LDS
+// buffers meanwhile, and the page ids of the one behind them into registers.
+// Up to 32 heads two workgroups of four waves share a compute unit, each with
+// one tile under way; more heads take eight waves' registers, and the one
+// workgroup keeps two tiles under way.
+constexpr int latent_waves(int head_tiles) { return head_tiles >= 4 ? 8 : 4; }
+constexpr int latent_ahead(int head_tiles) { return head_tiles >= 4 ? 2 : 1; }
 constexpr float kHeadroom = 60.0f;
 
 template <int R, int P, int NHT>
@@ -242,12 +245,15 @@ __global__ __launch_bounds__(64 * latent_waves(NHT), 2) void latent_attn_kernel(
   using PG = LatentPage<R, P>;
   constexpr int NW = latent_waves(NHT), T = 64 * NW;
   constexpr int KI = PG::KI, DT = R / (16 * NW);   // score steps; 16-element output tiles of a wave
-  constexpr int JP = NHT <= 2 ? 1 : 2;             // pages per scoring wave
+  constexpr int JP = 2 * NHT <= NW ? 1 : 2;        // pages per scoring wave
+  constexpr int D = latent_ahead(NHT);             // tiles under way
+  constexpr int kQl = R >= 512 && NHT >= 8 ? 4 : 0;            // score steps whose queries stay in LDS: registers are full
   constexpr int QW = NHT * 2 / JP;                 // scoring waves
   static_assert(QW <= NW, "a wave per score job");
   __shared__ __align__(16) struct {
-    uint8_t tile[2][2 * PG::kHiBytes];
+    uint8_t tile[D + 1][2 * PG::kHiBytes];
     uint8_t p[NHT * 1024];
+    uint8_t q[kQl > 0 ? NHT * kQl * 1024 : 16];
     long long scan[NW + 2];
     float top[QW * 16], sum[QW * 16], alpha[NHT * 16];
     int grown[QW];
@@ -268,50 +274,59 @@ __global__ __launch_bounds__(64 * latent_waves(NHT), 2) void latent_attn_kernel(
   const int v_at = (e * 16 + ((4 * q4 + (n >> 2)) ^ (8 * e))) * 16 + 8 * (n & 1) + wave * DT * 512;
   const int k_at = (16 * q4 + latent_swap(q4, n)) * 16 + page0 * PG::kHiBytes;
 
-  // The walk over the list: the current tile, the next (its page ids known) and
-  // the one after it (its page ids under way), and the counts of the sequence
-  // behind that one.
-  struct Place {
-    Seq s;
-    int j;
+  // The walk over the list: the current tile, those under way, and the one
+  // behind them, whose page ids are.
+  struct Item {
+    int b, m;                                      // sequence; slots (0: the tile of an empty sequence)
+    bool high, last;                               // of the HIGH store; the sequence's last tile
+    int p0, p1;                                    // pages (p1 negative: none), not looked at before they are needed
   };
-  struct Pages {
-    int p0, p1;
-  };
-  Counts ahead;
-  auto pages_of = [&](const Place& x) {
-    Pages g{0, -1};
-    const int m = x.s.slots(x.j);
-    if (m > 0) {
-      const bool high = x.j < x.s.nt_hi;
-      const int32_t* bt = block_table_of(cv, x.s.b, a.layer, high ? kHi : kLo) + 2 * (high ? x.j : x.j - x.s.nt_hi);
-      g.p0 = bt[0];
-      if (m > kPage) g.p1 = bt[1];
+  Seq walk = seq_of(place.b, counts_at(a, place.b));
+  int walk_j = (int)(u0 - place.start);
+  Counts ahead = counts_at(a, place.b + 1);        // of the sequence behind the walk's
+  auto next_item = [&]() {
+    Item x;
+    x.b = walk.b;
+    x.high = walk_j < walk.nt_hi;
+    const int k = x.high ? walk_j : walk_j - walk.nt_hi;
+    x.m = max(0, min(kTile, (x.high ? walk.n_hi : walk.n_lo) - k * kTile));
+    x.p0 = 0;
+    x.p1 = -1;
+    if (x.m > 0) {
+      const int32_t* bt = block_table_of(cv, walk.b, a.layer, x.high ? kHi : kLo) + 2 * k;
+      x.p0 = bt[0];
+      if (x.m > kPage) x.p1 = bt[1];
     }
-    return g;
-  };
-  auto after = [&](const Place& x) {
-    Place y = x;
-    if (++y.j == y.s.nt) {
-      y.s = seq_of(x.s.b + 1, ahead);
-      y.j = 0;
-      ahead = counts_at(a, y.s.b + 1);
+    x.last = ++walk_j == walk.nt;
+    if (x.last) {
+      walk = seq_of(walk.b + 1, ahead);
+      walk_j = 0;
+      ahead = counts_at(a, walk.b + 1);
     }
-    return y;
+    return x;
   };
   using TL = Tile<R, P, T>;
-  auto fetch = [&](const Place& x, const Pages& g, uint8_t* tile) {
-    if (x.s.slots(x.j) <= 0) return;
-    if (x.j < x.s.nt_hi) TL::copy_high(cv.hi_pool, uni(g.p0), uni(g.p1), tile, wave, lane);
-    else TL::copy_low(cv.lo_pool, uni(g.p0), uni(g.p1), tile, wave, lane);
+  bool long_wait = true;                           // the newest copies are not a full HIGH tile's
+  auto fetch = [&](const Item& x, uint8_t* tile) {
+    const int p1 = uni(x.p1);
+    if (x.m > 0) {
+      if (x.high) TL::copy_high(cv.hi_pool, uni(x.p0), p1, tile, wave, lane);
+      else TL::copy_low(cv.lo_pool, uni(x.p0), p1, tile, wave, lane);
+    }
+    long_wait = !x.high || p1 < 0;
   };
-  uint4 qf[KI];
+  uint4 qf[KI - kQl];
+  const uint32_t q_at = lds_address(sm.q) + (ht * kQl * 64 + lane) * 16;
   auto load_queries = [&](int b) {
-    const int head = ht * 16 + n;
-    const uint16_t* src = a.q + ((size_t)b * a.heads + head) * (R + P) + 8 * q4;
+    const int l = fresh(lane), head = ht * 16 + (l & 15);
+    const uint16_t* src = a.q + ((size_t)b * a.heads + head) * (R + P) + 8 * (l >> 4);
 #pragma unroll
-    for (int i = 0; i < KI; ++i)
-      qf[i] = scores && head < a.heads ? *reinterpret_cast<const uint4*>(src + 32 * i) : make_uint4(0u, 0u, 0u, 0u);
+    for (int i = 0; i < KI; ++i) {
+      const uint4 x =
+          scores && head < a.heads ? *reinterpret_cast<const uint4*>(src + 32 * i) : make_uint4(0u, 0u, 0u, 0u);
+      if (i >= kQl) qf[i - kQl] = x;
+      else if (scores) write_lds16(q_at + i * 1024, x);
+    }
   };
   f32x4_t acc[NHT][DT];
   float x[4 * JP], mx, sum, part = 0.0f, top = -INFINITY;      // scaled scores of the tile, reference, sums
@@ -339,9 +354,9 @@ __global__ __launch_bounds__(64 * latent_waves(NHT), 2) void latent_attn_kernel(
   };
   // Scores and weights of a tile in LDS; true for every wave if some head's
   // reference has to move first (move_reference).
-  auto score = [&](const Place& at, uint8_t* tile) {
-    const int m = at.s.slots(at.j);
-    if (at.j >= at.s.nt_hi && m > 0) {
+  auto score = [&](const Item& at, uint8_t* tile) {
+    const int m = at.m;
+    if (!at.high && m > 0) {
       TL::widen_low(tile, m);
     } else if (m < kTile) {                        // a HIGH store's last tile, or an empty sequence's
       TL::clear_from(tile, m);
@@ -355,7 +370,8 @@ __global__ __launch_bounds__(64 * latent_waves(NHT), 2) void latent_attn_kernel(
       for (int i = 0; i < KI; ++i)
 #pragma unroll
         for (int jp = 0; jp < JP; ++jp)
-          s[jp] = mfma(read_lds16(lds_address(tile) + jp * PG::kHiBytes + i * 1024 + k_at), qf[i], s[jp]);
+          s[jp] = mfma(read_lds16(lds_address(tile) + jp * PG::kHiBytes + i * 1024 + k_at),
+                       i >= kQl ? qf[i - kQl] : read_lds16(q_at + i * 1024), s[jp]);
       top = -INFINITY;
 #pragma unroll
       for (int r = 0; r < 4 * JP; ++r) {
@@ -416,65 +432,63 @@ __global__ __launch_bounds__(64 * latent_waves(NHT), 2) void latent_attn_kernel(
     if constexpr (DT > 4) four(std::integral_constant<int, 4>{});
   };
 
-  Place cur, next, later;
-  Pages next_pages, later_pages;
-  ahead = counts_at(a, place.b + 1);
-  cur.s = seq_of(place.b, counts_at(a, place.b));
-  cur.j = (int)(u0 - place.start);
-  long long start = place.start, u = u0;           // the list's tile 0 of cur.s; cur's place in the list
-  const Pages first = pages_of(cur);
-  next = cur;
-  next_pages = first;
-  if (u + 1 < u1) {
-    next = after(cur);
-    next_pages = pages_of(next);
-  }
-  later = next;
-  later_pages = next_pages;
-  int buf = 0;
-  load_queries(cur.s.b);
+  long long start = place.start, u = u0;           // tile 0 of the current sequence; the current tile
+  Item item[D + 2];                                // tiles u .. u + D + 1 (the last of them from look_ahead on)
+#pragma unroll
+  for (int k = 0; k < D + 2; ++k)
+    if (k == 0 || (k <= D && u + k < u1)) item[k] = next_item();
+    else item[k] = item[k - 1];
+  int buf = 0;                                     // of the current tile
+  auto buffer = [&](int k) {
+    const int x = buf + k;
+    return sm.tile[x > D ? x - D - 1 : x];
+  };
+  load_queries(item[0].b);
   restart();
-  fetch(cur, first, sm.tile[0]);
+#pragma unroll
+  for (int k = 0; k < D; ++k)
+    if (u + k < u1) fetch(item[k], buffer(k));
   wait_loads();
   __syncthreads();
-  // Everything of the tile before is done with: the next tile on its way into
-  // the free buffer, the page ids of the one after it.
+  // With every wave done with the tile before: a tile on its way into its
+  // buffer, and ahead of it the page ids of the next one (loads return in order).
   auto look_ahead = [&]() {
-    if (u + 1 < u1) fetch(next, next_pages, sm.tile[buf ^ 1]);
-    if (u + 2 < u1) {
-      later = after(next);
-      later_pages = pages_of(later);
-    }
+    const Item x = item[D];
+    if (u + D + 1 < u1) item[D + 1] = next_item();
+    if (u + D < u1) fetch(x, buffer(D));
   };
   auto advance = [&]() {
-    cur = next;
-    next = later;
-    next_pages = later_pages;
+#pragma unroll
+    for (int k = 0; k <= D; ++k) item[k] = item[k + 1];
     ++u;
-    buf ^= 1;
-    wait_loads();
-    __syncthreads();
+    buf = buf == D ? 0 : buf + 1;
+    // The next tile has arrived when only the newest one's copies are under way.
+    constexpr int kNewest = 2 * PG::KI / NW;       // at least, of each wave
+    static_assert(kNewest < 16, "in the counter's low bits");
+    if (D == 1 || long_wait || u + D > u1) wait_loads();
+    else __builtin_amdgcn_s_waitcnt(0x0F70 | kNewest);
+    lds_barrier();
   };
   look_ahead();
-  bool grown = score(cur, sm.tile[buf]);
+  bool grown = score(item[0], sm.tile[0]);
   for (;;) {
     if (grown) move_reference();
     bool ends;
     for (;;) {                                     // tiles of one sequence, until a reference has to move
       sum += part;
       add_values(sm.tile[buf]);
-      ends = cur.j + 1 == cur.s.nt || u + 1 == u1;             // the worker's last tile of this sequence
+      ends = item[0].last || u + 1 == u1;          // the worker's last tile of this sequence
       if (ends) break;
       advance();
       look_ahead();
-      grown = score(cur, sm.tile[buf]);
+      grown = score(item[0], sm.tile[buf]);
       if (grown) break;
     }
     if (!ends) continue;
 
     // Results: the whole history, or a part of it in slot 2w (the worker's
     // first sequence) or 2w + 1 of the partials.
-    const Seq s = cur.s;
+    const Seq s = seq_of(item[0].b, counts_at(a, item[0].b));
     const bool whole = start >= u0 && start + s.nt <= u1;
     const int slot = 2 * (int)blockIdx.x + (start > u0 ? 1 : 0);
     if (threadIdx.x == 0 && start >= u0) {
@@ -501,16 +515,17 @@ __global__ __launch_bounds__(64 * latent_waves(NHT), 2) void latent_attn_kernel(
       }
     }
     const bool more = u + 1 < u1;
-    if (more) load_queries(next.s.b);
+    if (more) load_queries(item[1].b);
     lds_barrier();
+    const int l = fresh(lane);
 #pragma unroll
     for (int h = 0; h < NHT; ++h) {
-      const int head = h * 16 + n;
+      const int head = h * 16 + (l & 15);
       if (head < a.heads) {
         const float inv = sm.alpha[head];
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
-          const int dim = 16 * (wave * DT + d) + 4 * q4;
+          const int dim = 16 * (wave * DT + d) + 4 * (l >> 4);
           const f32x4_t o = acc[h][d];
           if (whole) {
             *reinterpret_cast<uint2*>(a.out + ((size_t)s.b * a.heads + head) * R + dim) =
@@ -524,9 +539,10 @@ __global__ __launch_bounds__(64 * latent_waves(NHT), 2) void latent_attn_kernel(
     if (!more) return;
     start += s.nt;
     restart();
+    long_wait = true;                              // results have been stored since
     advance();
     look_ahead();
-    grown = score(cur, sm.tile[buf]);
+    grown = score(item[0], sm.tile[buf]);
   }
 }
 
@@ -607,7 +623,7 @@ void launch_heads(const LatentAttnArgs& a, hipStream_t s) {
 int latent_workers(int rank, int rope, int heads, int64_t tiles) {
   (void)rank;
   (void)rope;
-  const int resident = latent_head_tiles(heads) >= 8 ? 256 : 512;
+  const int resident = latent_head_tiles(heads) >= 4 ? 256 : 512;
   return (int)std::max<int64_t>(1, std::min<int64_t>(resident, tiles));
 }
 

@@ -46,6 +46,14 @@ __device__ __forceinline__ uint4 low_values(uint32_t w, float s) {
 }
 __device__ __forceinline__ float half_value(uint16_t h) { return (float)__builtin_bit_cast(_Float16, h); }
 
+// x, which the compiler takes for new (no code): what follows from it is made
+// where it is used, not kept in registers through the loops around.
+template <typename I>
+__device__ __forceinline__ I fresh(I x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
 // Transposing reads of LDS (ds_read_b64_tr_b16): of each 16 lanes, lanes 4r ..
 // 4r + 3 address row r's four 8-byte quarters (4 rows of 16 2-byte elements),
 // and lane i receives element i of the rows.  Four pairs of reads at a time,

@@ -162,10 +162,6 @@ __global__ __launch_bounds__(64 * W, 2) void latent_prompt_kernel(LatentPromptAr
   const uint32_t kr_at = (uint32_t)(kKn + (n * PC + key_swap<PC>(n, g)) * 16);
   const uint32_t v_at = (uint32_t)(kKn + kKr + (v_row * VC + value_swap<VC>(v_row, 2 * ((lane >> 4) & 1) + ((l16 & 3) >> 1))) * 16 +
                                    8 * (l16 & 1));
-  auto fresh = [](uint32_t x) {                    // no code: addresses are made where they are used, not kept in registers
-    asm volatile("" : "+v"(x));
-    return x;
-  };
   auto scores = [&](uint32_t kvs, int u) {         // of keys 32 u .. of the step at LDS address kvs
     f32x16_t s;
 #pragma unroll
