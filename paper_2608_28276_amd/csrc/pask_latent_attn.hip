@@ -363,15 +363,32 @@ __global__ __launch_bounds__(64 * latent_waves(NHT), 2) void latent_attn_kernel(
       lds_barrier();
     }
     if (scores) {
-      f32x4_t s[JP];
+      // Two sums at a time (the two pages, or even and odd steps of one), the
+      // operands of kAhead steps read in advance: in pinned order, as left to
+      // itself the compiler saves registers and waits for every read.
+      constexpr int kAhead = JP == 1 ? 6 : (NHT >= 8 ? 2 : 3);
+      const uint32_t kb = fresh(lds_address(tile) + k_at);
+      auto operand = [&](int i, int jp) { return read_lds16(kb + jp * PG::kHiBytes + i * 1024); };
+      f32x4_t s[2] = {f32x4_t{0.0f, 0.0f, 0.0f, 0.0f}, f32x4_t{0.0f, 0.0f, 0.0f, 0.0f}};
+      uint4 kf[kAhead][JP], ql[kQl > 0 ? kQl : 1];
 #pragma unroll
-      for (int jp = 0; jp < JP; ++jp) s[jp] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+      for (int i = 0; i < kQl; ++i) ql[i] = read_lds16(q_at + i * 1024);
 #pragma unroll
-      for (int i = 0; i < KI; ++i)
+      for (int i = 0; i < kAhead; ++i)
 #pragma unroll
-        for (int jp = 0; jp < JP; ++jp)
-          s[jp] = mfma(read_lds16(lds_address(tile) + jp * PG::kHiBytes + i * 1024 + k_at),
-                       i >= kQl ? qf[i - kQl] : read_lds16(q_at + i * 1024), s[jp]);
+        for (int jp = 0; jp < JP; ++jp) kf[i][jp] = operand(i, jp);
+#pragma unroll
+      for (int i = 0; i < KI; ++i) {
+        const uint4 qi = i >= kQl ? qf[i - kQl] : ql[i];
+#pragma unroll
+        for (int jp = 0; jp < JP; ++jp) {
+          f32x4_t& to = s[JP == 1 ? i & 1 : jp];
+          to = mfma(kf[i % kAhead][jp], qi, to);
+          if (i + kAhead < KI) kf[i % kAhead][jp] = operand(i + kAhead, jp);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if constexpr (JP == 1) s[0] += s[1];
       top = -INFINITY;
 #pragma unroll
       for (int r = 0; r < 4 * JP; ++r) {
@@ -414,22 +431,24 @@ __global__ __launch_bounds__(64 * latent_waves(NHT), 2) void latent_attn_kernel(
     }
   };
   auto add_values = [&](const uint8_t* tile) {
-    const uint32_t vs = lds_address(tile) + v_at;
-    auto four = [&](auto first) {                  // output tiles first .. + 3 (those below DT)
-      constexpr int d0 = decltype(first)::value, k = d0 * 512;
-      constexpr int k1 = DT > d0 + 1 ? k + 512 : k, k2 = DT > d0 + 2 ? k + 1024 : k, k3 = DT > d0 + 3 ? k + 1536 : k;
-      uint4 v[4];
-      read_transposed<k, k1, k2, k3, PG::kHiBytes>(vs, vs, vs, vs, v);
+    const uint32_t vs = lds_address(tile) + v_at, ps = lds_address(sm.p) + lane * 16;
+    constexpr int kW = NHT < 4 ? NHT : 4;          // weights read in advance
+    uint4 w[kW], v[DT > 4 ? 8 : 4];
 #pragma unroll
-      for (int h = 0; h < NHT; ++h) {
-        const uint4 w = read_lds16(lds_address(sm.p) + (h * 64 + lane) * 16);
+    for (int h = 0; h < kW; ++h) w[h] = read_lds16(ps + h * 1024);
+    if constexpr (DT > 4) {
+      read_transposed8<PG::kHiBytes>(vs, v);
+    } else {
+      constexpr int k1 = DT > 1 ? 512 : 0, k2 = DT > 2 ? 1024 : 0, k3 = DT > 3 ? 1536 : 0;
+      read_transposed<0, k1, k2, k3, PG::kHiBytes>(vs, vs, vs, vs, v);
+    }
 #pragma unroll
-        for (int d = 0; d < 4; ++d)
-          if (d0 + d < DT) acc[h][d0 + d] = mfma(v[d], w, acc[h][d0 + d]);
-      }
-    };
-    four(std::integral_constant<int, 0>{});
-    if constexpr (DT > 4) four(std::integral_constant<int, 4>{});
+    for (int h = 0; h < NHT; ++h) {
+#pragma unroll
+      for (int d = 0; d < DT; ++d) acc[h][d] = mfma(v[d], w[h % kW], acc[h][d]);
+      if (h + kW < NHT) w[h % kW] = read_lds16(ps + (h + kW) * 1024);
+      __builtin_amdgcn_sched_barrier(0);
+    }
   };
 
   long long start = place.start, u = u0;           // tile 0 of the current sequence; the current tile
