@@ -69,7 +69,7 @@ typedef struct pask_latent_cache {
 /* Region offsets of a cache of this geometry, in the fields of pask.h's
  * layout (status, counters, block tables, index lists and cursors mean the
  * same; there is no window).  The pages, with q = (d mod 32) / 8 and
- * u = t XOR 8 (q mod 2) for element d of slot t:
+ * u = t XOR 12 (q mod 2) for element d of slot t:
  *   hi_page_bytes  16 (rank + rope_dim) 2: the 16-byte chunk of elements
  *                  32i + 8q .. + 7 of slot t is chunk 64 i + 16 q + u; the
  *                  rotary key follows the latent as elements rank + e

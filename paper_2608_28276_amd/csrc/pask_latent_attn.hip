@@ -271,7 +271,7 @@ __global__ __launch_bounds__(64 * latent_waves(NHT), 2) void latent_attn_kernel(
   const long long u0 = (long long)blockIdx.x * units, u1 = u0 + units < place.total ? u0 + units : place.total;
   if (u0 >= place.total) return;
   const int e = (n & 3) >> 1;                      // value operand: quarter, slot and half of a lane's 8 bytes
-  const int v_at = (e * 16 + ((4 * q4 + (n >> 2)) ^ (8 * e))) * 16 + 8 * (n & 1) + wave * DT * 512;
+  const int v_at = (e * 16 + latent_swap(e, 4 * q4 + (n >> 2))) * 16 + 8 * (n & 1) + wave * DT * 512;
   const int k_at = (16 * q4 + latent_swap(q4, n)) * 16 + page0 * PG::kHiBytes;
 
   // The walk over the list: the current tile, those under way, and the one

@@ -11,12 +11,14 @@ namespace {
 
 // Pages of 16 slots, laid out for the attention kernel, which copies a page
 // into LDS as it lies and uses the tile both as keys and as values:
-//   HIGH  16-byte chunks, chunk 64 i + 16 q + (t ^ 8 (q & 1)) holding elements
-//         32 i + 8 q .. + 7 of slot t (the rotary key follows the latent), so
-//         lane (q, t) of a score operand reads 1 KiB per wave contiguously, and
-//         the transposing reads of the value operand, which take 4 slots x 16
-//         elements per 16 lanes, fall on all banks (without the XOR the chunks
-//         of two neighbouring q would share them).
+//   HIGH  16-byte chunks, chunk 64 i + 16 q + (t ^ 12 (q & 1)) holding elements
+//         32 i + 8 q .. + 7 of slot t (the rotary key follows the latent).  A
+//         score operand is 1 KiB per wave; its reads take lanes 0-3, 12-15,
+//         20-23, 24-27 (and so on) at a time, which the XOR keeps on different
+//         banks, while the transposing reads of the value operand, 4 slots x 2
+//         chunks per 16 lanes, would without it find neighbouring q on the same
+//         ones (cycles per instruction and compute unit, keys / values: no XOR
+//         4.3 / 4, with 8 in place of 12 8.0 / 2, with 12 4.3 / 2).
 //   LOW   code words (16 i + t) * 4 + q of elements 32 i + 8 q .. + 7 (k_word
 //         order, offset binary): the 16 bytes and the scale of a 32-element
 //         group belong to one thread, in the write and in the attention's
@@ -32,7 +34,7 @@ struct LatentPage {
   static_assert(kLoBytes % 16 == 0 && kRopeAt % 16 == 0, "16-byte pieces");
 };
 // Slot t and its chunk position within a row of 16 chunks of quarter q.
-__host__ __device__ __forceinline__ constexpr int latent_swap(int q, int t) { return t ^ ((q & 1) << 3); }
+__host__ __device__ __forceinline__ constexpr int latent_swap(int q, int t) { return t ^ ((q & 1) * 12); }
 
 // The bf16 values of the 8 codes of a word under scale s, as 16 bytes in
 // element order: (n - 8) * s = fma(n, s, -8 s) is exact in fp32 (a code has 3

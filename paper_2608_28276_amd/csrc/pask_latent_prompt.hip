@@ -37,9 +37,9 @@ __device__ __forceinline__ f32x16_t mfma(uint4 a, uint4 b, f32x16_t c) {
 // (256 / (16 C) rows share the 64 banks).
 template <int C>
 __device__ __forceinline__ int key_swap(int t, int d) { return d ^ ((C >= 16 ? t : t / (16 / C)) & (C - 1)); }
-// The same for values, which the transposing reads take in pairs of chunks of 4 rows.
+// The same for values, which the transposing reads take 4 rows x 4 chunks at a time.
 template <int C>
-__device__ __forceinline__ int value_swap(int t, int d) { return d ^ ((t & (C / 2 - 1)) << 1); }
+__device__ __forceinline__ int value_swap(int t, int d) { return d ^ ((t / (16 / C) & (C / 4 - 1)) << 2); }
 
 // O += P V key by key over 32 keys (values at s_v), where a value that some
 // query does not see is infinite or NaN (a weight of 0 times it is not 0): only
