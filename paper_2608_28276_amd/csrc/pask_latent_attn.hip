@@ -40,27 +40,15 @@ __device__ __forceinline__ f32x4_t mfma(uint4 a, uint4 b, f32x4_t c) {
 // nothing (its worker writes the empty result).  Worker w of W takes tiles
 // [w u, w u + u), u = ceil(total / W).
 __device__ __forceinline__ int uni(int x) { return __builtin_amdgcn_readfirstlane(x); }
-struct Counts {                                    // as loaded: not looked at before they are needed
+struct Counts {
   int n_hi, n_lo;
 };
 __device__ __forceinline__ Counts counts_at(const LatentAttnArgs& a, int b) {
   const int32_t* c = counters_of(a.cv, min(b, a.batch - 1), a.layer);
   return Counts{c[kCntHi], c[kCntLo]};
 }
-struct Seq {
-  int b, n_hi, n_lo, nt_hi, nt;
-};
-__device__ __forceinline__ int tiles_of(int n_hi, int n_lo) {
-  return max(1, (n_hi + kTile - 1) / kTile + (n_lo + kTile - 1) / kTile);
-}
-__device__ __forceinline__ Seq seq_of(int b, const Counts& c) {
-  Seq s;
-  s.b = b;
-  s.n_hi = uni(c.n_hi);
-  s.n_lo = uni(c.n_lo);
-  s.nt_hi = (s.n_hi + kTile - 1) / kTile;
-  s.nt = tiles_of(s.n_hi, s.n_lo);
-  return s;
+__device__ __forceinline__ int tiles_of(const Counts& c) {
+  return max(1, (c.n_hi + kTile - 1) / kTile + (c.n_lo + kTile - 1) / kTile);
 }
 
 // Over the whole workgroup of T threads (thread t counts sequences [t B / T,
@@ -74,10 +62,7 @@ template <int T, typename At>
 __device__ __forceinline__ ListPlace find_in_list(const LatentAttnArgs& a, long long* s_scan, At at) {
   constexpr int kWaves = T / 64;
   const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  auto tiles = [&](int b) {
-    const Counts c = counts_at(a, b);
-    return tiles_of(c.n_hi, c.n_lo);
-  };
+  auto tiles = [&](int b) { return tiles_of(counts_at(a, b)); };
   long long mine = 0;
   const int first = (int)((long long)a.batch * tid / T), last = (int)((long long)a.batch * (tid + 1) / T);
   for (int b = first; b < last; ++b) mine += tiles(b);
@@ -115,6 +100,55 @@ __device__ __forceinline__ long long tiles_per_worker(long long total, int worke
   const int best = (int)sqrtf(76.0f * (float)total / (float)head_tiles) + 1;
   const int n = min(workers, best);
   return (total + n - 1) / n;
+}
+
+// The next 64 tiles of a worker, looked up by one wave at once (a chain of two
+// loads for all of them: page ids loaded tile by tile came, in the loads' order,
+// behind the copies of the tiles before).
+struct Item {
+  int b, what, p0, p1;                             // sequence; slots | flags; pages (p1 negative: none)
+  __device__ __forceinline__ int slots() const { return what & 63; }   // 0: the tile of an empty sequence
+  __device__ __forceinline__ bool high() const { return (what & 64) != 0; }    // of the HIGH store
+  __device__ __forceinline__ bool first() const { return (what & 128) != 0; }  // of its sequence
+  __device__ __forceinline__ bool last() const { return (what & 256) != 0; }
+};
+// Lane k: tile `at` + k of the list, whose tile `start` is the first of
+// sequence b (start <= at, and at is not behind the sequence).  The place to go
+// on from for tile at + 64 goes to b and start.
+__device__ __forceinline__ Item look_up(const LatentAttnArgs& a, long long at, int& b, long long& start) {
+  const int lane = fresh((int)threadIdx.x & 63);
+  const Counts c = counts_at(a, b + lane);         // 64 sequences have 64 tiles or more
+  const int nt = tiles_of(c);
+  int incl = nt;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const int y = __shfl_up(incl, off);
+    if (lane >= off) incl = min(incl + y, 1 << 30);
+  }
+  const int x = (int)(at - start) + lane;          // the lane's tile from `start` on
+  int lo = 0;                                      // the sequence that holds it: the first with incl > x
+#pragma unroll
+  for (int step = 32; step > 0; step >>= 1)
+    if (__shfl(incl, lo + step - 1) <= x) lo += step;
+  const int behind = __shfl(incl, lo), n = __shfl(nt, lo), j = x - (behind - n);
+  const Counts s{__shfl(c.n_hi, lo), __shfl(c.n_lo, lo)};
+  Item it;
+  it.b = b + lo;
+  const int nt_hi = (s.n_hi + kTile - 1) / kTile;
+  const bool high = j < nt_hi;
+  const int k = high ? j : j - nt_hi, m = max(0, min(kTile, (high ? s.n_hi : s.n_lo) - k * kTile));
+  it.what = m | (high ? 64 : 0) | (j == 0 ? 128 : 0) | (j + 1 == n ? 256 : 0);
+  it.p0 = 0;
+  it.p1 = -1;
+  if (it.b < a.batch && m > 0) {                   // tiles behind the list's last are not used
+    const int32_t* bt = block_table_of(a.cv, it.b, a.layer, high ? kHi : kLo) + 2 * k;
+    it.p0 = bt[0];
+    if (m > kPage) it.p1 = bt[1];
+  }
+  const bool ended = j + 1 == n;
+  b = __builtin_amdgcn_readlane(ended ? it.b + 1 : it.b, 63);
+  start += __builtin_amdgcn_readlane(ended ? behind : behind - n, 63);
+  return it;
 }
 
 // ---------------------------------------------------------------------------
@@ -255,6 +289,7 @@ __global__ __launch_bounds__(64 * latent_waves(NHT), 2) void latent_attn_kernel(
     uint8_t p[NHT * 1024];
     uint8_t q[kQl > 0 ? NHT * kQl * 1024 : 16];
     long long scan[NW + 2];
+    uint8_t item[128 * 16];
     float top[QW * 16], sum[QW * 16], alpha[NHT * 16];
     int grown[QW];
   } sm;
@@ -274,46 +309,29 @@ __global__ __launch_bounds__(64 * latent_waves(NHT), 2) void latent_attn_kernel(
   const int v_at = (e * 16 + latent_swap(e, 4 * q4 + (n >> 2))) * 16 + 8 * (n & 1) + wave * DT * 512;
   const int k_at = (16 * q4 + latent_swap(q4, n)) * 16 + page0 * PG::kHiBytes;
 
-  // The walk over the list: the current tile, those under way, and the one
-  // behind them, whose page ids are.
-  struct Item {
-    int b, m;                                      // sequence; slots (0: the tile of an empty sequence)
-    bool high, last;                               // of the HIGH store; the sequence's last tile
-    int p0, p1;                                    // pages (p1 negative: none), not looked at before they are needed
+  // The table of the worker's tiles, 64 at a time: entry (tile - u0) mod 128.
+  int walk_b = place.b;
+  long long walk_start = place.start;
+  auto fill = [&](long long at) {                  // tiles at .. at + 63
+    if (wave == 0) {
+      const Item x = look_up(a, at, walk_b, walk_start);
+      write_lds16(lds_address(sm.item) + (((int)(at - u0) & 64) + fresh(lane)) * 16,
+                  make_uint4((uint32_t)x.b, (uint32_t)x.what, (uint32_t)x.p0, (uint32_t)x.p1));
+    }
+    lds_barrier();
   };
-  Seq walk = seq_of(place.b, counts_at(a, place.b));
-  int walk_j = (int)(u0 - place.start);
-  Counts ahead = counts_at(a, place.b + 1);        // of the sequence behind the walk's
-  auto next_item = [&]() {
-    Item x;
-    x.b = walk.b;
-    x.high = walk_j < walk.nt_hi;
-    const int k = x.high ? walk_j : walk_j - walk.nt_hi;
-    x.m = max(0, min(kTile, (x.high ? walk.n_hi : walk.n_lo) - k * kTile));
-    x.p0 = 0;
-    x.p1 = -1;
-    if (x.m > 0) {
-      const int32_t* bt = block_table_of(cv, walk.b, a.layer, x.high ? kHi : kLo) + 2 * k;
-      x.p0 = bt[0];
-      if (x.m > kPage) x.p1 = bt[1];
-    }
-    x.last = ++walk_j == walk.nt;
-    if (x.last) {
-      walk = seq_of(walk.b + 1, ahead);
-      walk_j = 0;
-      ahead = counts_at(a, walk.b + 1);
-    }
-    return x;
+  auto item = [&](long long u) {
+    const uint4 x = read_lds16(lds_address(sm.item) + ((int)(u - u0) & 127) * 16);
+    return Item{uni((int)x.x), uni((int)x.y), uni((int)x.z), uni((int)x.w)};
   };
   using TL = Tile<R, P, T>;
   bool long_wait = true;                           // the newest copies are not a full HIGH tile's
   auto fetch = [&](const Item& x, uint8_t* tile) {
-    const int p1 = uni(x.p1);
-    if (x.m > 0) {
-      if (x.high) TL::copy_high(cv.hi_pool, uni(x.p0), p1, tile, wave, lane);
-      else TL::copy_low(cv.lo_pool, uni(x.p0), p1, tile, wave, lane);
+    if (x.slots() > 0) {
+      if (x.high()) TL::copy_high(cv.hi_pool, x.p0, x.p1, tile, wave, lane);
+      else TL::copy_low(cv.lo_pool, x.p0, x.p1, tile, wave, lane);
     }
-    long_wait = !x.high || p1 < 0;
+    long_wait = !x.high() || x.p1 < 0;
   };
   uint4 qf[KI - kQl];
   const uint32_t q_at = lds_address(sm.q) + (ht * kQl * 64 + lane) * 16;
@@ -324,8 +342,8 @@ __global__ __launch_bounds__(64 * latent_waves(NHT), 2) void latent_attn_kernel(
     for (int i = 0; i < KI; ++i) {
       const uint4 x =
           scores && head < a.heads ? *reinterpret_cast<const uint4*>(src + 32 * i) : make_uint4(0u, 0u, 0u, 0u);
-      if (i >= kQl) qf[i - kQl] = x;
-      else if (scores) write_lds16(q_at + i * 1024, x);
+      if (i < KI - kQl) qf[i] = x;
+      else if (scores) write_lds16(fresh(q_at) + (i - KI + kQl) * 1024, x);
     }
   };
   f32x4_t acc[NHT][DT];
@@ -355,8 +373,8 @@ __global__ __launch_bounds__(64 * latent_waves(NHT), 2) void latent_attn_kernel(
   // Scores and weights of a tile in LDS; true for every wave if some head's
   // reference has to move first (move_reference).
   auto score = [&](const Item& at, uint8_t* tile) {
-    const int m = at.m;
-    if (!at.high && m > 0) {
+    const int m = at.slots();
+    if (!at.high() && m > 0) {
       TL::widen_low(tile, m);
     } else if (m < kTile) {                        // a HIGH store's last tile, or an empty sequence's
       TL::clear_from(tile, m);
@@ -370,22 +388,23 @@ __global__ __launch_bounds__(64 * latent_waves(NHT), 2) void latent_attn_kernel(
       const uint32_t kb = fresh(lds_address(tile) + k_at);
       auto operand = [&](int i, int jp) { return read_lds16(kb + jp * PG::kHiBytes + i * 1024); };
       f32x4_t s[2] = {f32x4_t{0.0f, 0.0f, 0.0f, 0.0f}, f32x4_t{0.0f, 0.0f, 0.0f, 0.0f}};
-      uint4 kf[kAhead][JP], ql[kQl > 0 ? kQl : 1];
-#pragma unroll
-      for (int i = 0; i < kQl; ++i) ql[i] = read_lds16(q_at + i * 1024);
+      // Steps whose queries are in LDS come last.
+      auto queries = [&](int i) { return i < KI - kQl ? qf[i] : read_lds16(q_at + (i - KI + kQl) * 1024); };
+      uint4 kf[kAhead][JP], ql[2];
 #pragma unroll
       for (int i = 0; i < kAhead; ++i)
 #pragma unroll
         for (int jp = 0; jp < JP; ++jp) kf[i][jp] = operand(i, jp);
 #pragma unroll
       for (int i = 0; i < KI; ++i) {
-        const uint4 qi = i >= kQl ? qf[i - kQl] : ql[i];
+        const uint4 qi = i < KI - kQl ? qf[i] : ql[i & 1];
 #pragma unroll
         for (int jp = 0; jp < JP; ++jp) {
           f32x4_t& to = s[JP == 1 ? i & 1 : jp];
           to = mfma(kf[i % kAhead][jp], qi, to);
           if (i + kAhead < KI) kf[i % kAhead][jp] = operand(i + kAhead, jp);
         }
+        if (kQl > 0 && i + 2 >= KI - kQl && i + 2 < KI) ql[i & 1] = queries(i + 2);
         __builtin_amdgcn_sched_barrier(0);
       }
       if constexpr (JP == 1) s[0] += s[1];
@@ -451,34 +470,28 @@ __global__ __launch_bounds__(64 * latent_waves(NHT), 2) void latent_attn_kernel(
     }
   };
 
-  long long start = place.start, u = u0;           // tile 0 of the current sequence; the current tile
-  Item item[D + 2];                                // tiles u .. u + D + 1 (the last of them from look_ahead on)
-#pragma unroll
-  for (int k = 0; k < D + 2; ++k)
-    if (k == 0 || (k <= D && u + k < u1)) item[k] = next_item();
-    else item[k] = item[k - 1];
-  int buf = 0;                                     // of the current tile
+  long long u = u0, seq_u = u0;                    // the current tile; the first here of its sequence
+  int buf = 0;                                     // its buffer
   auto buffer = [&](int k) {
     const int x = buf + k;
     return sm.tile[x > D ? x - D - 1 : x];
   };
-  load_queries(item[0].b);
+  fill(u0);
+  Item cur = item(u0);
+  load_queries(cur.b);
   restart();
 #pragma unroll
   for (int k = 0; k < D; ++k)
-    if (u + k < u1) fetch(item[k], buffer(k));
+    if (u + k < u1) fetch(item(u + k), buffer(k));
   wait_loads();
   __syncthreads();
-  // With every wave done with the tile before: a tile on its way into its
-  // buffer, and ahead of it the page ids of the next one (loads return in order).
+  // With every wave done with the tile before: a tile on its way into its buffer.
   auto look_ahead = [&]() {
-    const Item x = item[D];
-    if (u + D + 1 < u1) item[D + 1] = next_item();
-    if (u + D < u1) fetch(x, buffer(D));
+    if (u + D >= u1) return;
+    if (((u + D - u0) & 63) == 0) fill(u + D);
+    fetch(item(u + D), buffer(D));
   };
   auto advance = [&]() {
-#pragma unroll
-    for (int k = 0; k <= D; ++k) item[k] = item[k + 1];
     ++u;
     buf = buf == D ? 0 : buf + 1;
     // The next tile has arrived when only the newest one's copies are under way.
@@ -487,32 +500,40 @@ __global__ __launch_bounds__(64 * latent_waves(NHT), 2) void latent_attn_kernel(
     if (D == 1 || long_wait || u + D > u1) wait_loads();
     else __builtin_amdgcn_s_waitcnt(0x0F70 | kNewest);
     lds_barrier();
+    cur = item(u);
   };
   look_ahead();
-  bool grown = score(item[0], sm.tile[0]);
+  bool grown = score(cur, sm.tile[0]);
+  bool later = false, begun = cur.first();         // not the worker's first sequence; the sequence's first tile was here
   for (;;) {
     if (grown) move_reference();
     bool ends;
     for (;;) {                                     // tiles of one sequence, until a reference has to move
       sum += part;
       add_values(sm.tile[buf]);
-      ends = item[0].last || u + 1 == u1;          // the worker's last tile of this sequence
+      ends = cur.last() || u + 1 == u1;            // the worker's last tile of this sequence
       if (ends) break;
       advance();
       look_ahead();
-      grown = score(item[0], sm.tile[buf]);
+      grown = score(cur, sm.tile[buf]);
       if (grown) break;
     }
     if (!ends) continue;
 
     // Results: the whole history, or a part of it in slot 2w (the worker's
     // first sequence) or 2w + 1 of the partials.
-    const Seq s = seq_of(item[0].b, counts_at(a, item[0].b));
-    const bool whole = start >= u0 && start + s.nt <= u1;
-    const int slot = 2 * (int)blockIdx.x + (start > u0 ? 1 : 0);
-    if (threadIdx.x == 0 && start >= u0) {
-      a.ws_seq[2 * s.b] = slot;
-      a.ws_seq[2 * s.b + 1] = whole ? 0 : (int)((start + s.nt - 1) / units) - (int)blockIdx.x + 1;
+    const int b = cur.b;
+    const bool whole = begun && cur.last();
+    const int slot = 2 * (int)blockIdx.x + (later ? 1 : 0);
+    if (threadIdx.x == 0 && begun) {
+      int parts = 0;
+      if (!whole) {                                // it goes on to u1 and further
+        const Counts c = counts_at(a, b);
+        const long long rest = tiles_of(c) - (u + 1 - seq_u);
+        parts = 1 + (int)((rest + units - 1) / units);
+      }
+      a.ws_seq[2 * b] = slot;
+      a.ws_seq[2 * b + 1] = parts;
     }
     if (scores) {
       sum += __shfl_xor(sum, 16);
@@ -526,7 +547,7 @@ __global__ __launch_bounds__(64 * latent_waves(NHT), 2) void latent_attn_kernel(
       sm.alpha[head] = sum == 0.0f ? 0.0f : 1.0f / sum;
       if (whole) {
         if (a.lse && head < a.heads)
-          a.lse[(size_t)s.b * a.heads + head] = sum == 0.0f ? -INFINITY : (mx + __builtin_amdgcn_logf(sum)) * kLn2;
+          a.lse[(size_t)b * a.heads + head] = sum == 0.0f ? -INFINITY : (mx + __builtin_amdgcn_logf(sum)) * kLn2;
       } else {
         float* ml = a.ws_ml + ((size_t)slot * NHT * 16 + head) * 2;
         ml[0] = mx;
@@ -534,7 +555,7 @@ __global__ __launch_bounds__(64 * latent_waves(NHT), 2) void latent_attn_kernel(
       }
     }
     const bool more = u + 1 < u1;
-    if (more) load_queries(item[1].b);
+    if (more) load_queries(item(u + 1).b);
     lds_barrier();
     const int l = fresh(lane);
 #pragma unroll
@@ -547,7 +568,7 @@ __global__ __launch_bounds__(64 * latent_waves(NHT), 2) void latent_attn_kernel(
           const int dim = 16 * (wave * DT + d) + 4 * (l >> 4);
           const f32x4_t o = acc[h][d];
           if (whole) {
-            *reinterpret_cast<uint2*>(a.out + ((size_t)s.b * a.heads + head) * R + dim) =
+            *reinterpret_cast<uint2*>(a.out + ((size_t)b * a.heads + head) * R + dim) =
                 make_uint2(pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv));
           } else {
             *reinterpret_cast<f32x4_t*>(a.ws_o + ((size_t)slot * NHT * 16 + head) * R + dim) = o;
@@ -556,12 +577,14 @@ __global__ __launch_bounds__(64 * latent_waves(NHT), 2) void latent_attn_kernel(
       }
     }
     if (!more) return;
-    start += s.nt;
     restart();
     long_wait = true;                              // results have been stored since
     advance();
+    later = true;
+    begun = true;
+    seq_u = u;
     look_ahead();
-    grown = score(item[0], sm.tile[buf]);
+    grown = score(cur, sm.tile[buf]);
   }
 }
 
