@@ -16,26 +16,30 @@
 namespace pask {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kWaves = kThreads / 64;
 
-// The int4 codes of a 32-element group (x[q]: elements 8q .. 8q + 7) in page
-// order, and its scale's bits.
-__device__ __forceinline__ uint4 low_group(const uint4 (&x)[4], uint16_t& sbits) {
-  uint32_t mb = 0u;
-#pragma unroll
-  for (int q = 0; q < 4; ++q) mb = max(mb, abs_max_bits8(x[q]));
+// A 16-byte piece of an entry: step i (32 elements), quarter q of it (8
+// elements), slot t of the page.  Thread by thread in this order neighbours
+// touch 64 bytes of a row, and a wave all of step i in a page.
+struct Piece {
+  int i, q, t;
+};
+__device__ __forceinline__ Piece piece(int x) { return Piece{x >> 6, x & 3, (x >> 2) & 15}; }
+// Its chunk in a HIGH page, and in the rotary keys of either (i from 0 there).
+__device__ __forceinline__ int chunk_of(const Piece& p) { return 64 * p.i + 16 * p.q + latent_swap(p.q, p.t); }
+
+// The int4 codes of a quarter, in page order, with the scale of the 32
+// elements that this lane and the three beside it hold.
+__device__ __forceinline__ uint32_t low_word(const uint4& x, uint16_t& sbits) {
+  uint32_t mb = abs_max_bits8(x);
+  mb = max(mb, (uint32_t)__shfl_xor((int)mb, 1));
+  mb = max(mb, (uint32_t)__shfl_xor((int)mb, 2));
   float s, inv;
   bool plain;
   sbits = quant_scale_bf16(__uint_as_float(mb << 16), s, inv, plain);
-  uint32_t w[4];
-#pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    uint32_t cb[8];
-    code_bytes8(x[q], s, inv, plain, cb);
-    w[q] = low_bytes4((cb[4] << 4) | cb[0], (cb[5] << 4) | cb[1], (cb[6] << 4) | cb[2],
-                      (cb[7] << 4) | cb[3]);
-  }
-  return make_uint4(w[0], w[1], w[2], w[3]);
+  uint32_t cb[8];
+  code_bytes8(x, s, inv, plain, cb);
+  return low_bytes4((cb[4] << 4) | cb[0], (cb[5] << 4) | cb[1], (cb[6] << 4) | cb[2], (cb[7] << 4) | cb[3]);
 }
 
 // Block (k, b) fills page k of the pages of sequence b that this call's slots
@@ -72,34 +76,35 @@ __global__ __launch_bounds__(kThreads) void latent_pack_kernel(AppendArgs a) {
   __syncthreads();
   const uint16_t* c = a.k + (size_t)b * a.max_new * R;
   const uint16_t* r = a.v + (size_t)b * a.max_new * P;
-  auto rope_chunk = [&](int x, uint8_t* dst) {     // chunk x of the page's rotary keys
-    const int q = (x >> 4) & 3, t = latent_swap(q, x & 15), j = s_src[t];
-    if (j < 0) return;
-    *reinterpret_cast<uint4*>(dst + x * 16) =
-        *reinterpret_cast<const uint4*>(r + (size_t)j * P + 32 * (x >> 6) + 8 * q);
-  };
-  if (st == kHi) {
-    uint8_t* pg = cv.hi_pool + (size_t)page * PG::kHiBytes;
-    for (int x = tid; x < 64 * PG::RI; x += kThreads) {
-      const int q = (x >> 4) & 3, t = latent_swap(q, x & 15), j = s_src[t];
-      if (j >= 0)
-        *reinterpret_cast<uint4*>(pg + x * 16) =
-            *reinterpret_cast<const uint4*>(c + (size_t)j * R + 32 * (x >> 6) + 8 * q);
+  uint8_t* pg = st == kHi ? cv.hi_pool + (size_t)page * PG::kHiBytes : cv.lo_pool + (size_t)page * PG::kLoBytes;
+  uint8_t* rope = pg + (st == kHi ? 1024 * PG::RI : PG::kRopeAt);
+  constexpr int kItems = (PG::KI + kWaves - 1) / kWaves;
+  uint4 v[kItems];                                 // all loads before the first store
+#pragma unroll
+  for (int u = 0; u < kItems; ++u) {
+    const Piece p = piece(tid + u * kThreads);
+    const int j = p.i < PG::KI ? s_src[p.t] : -1;
+    const uint16_t* src = p.i < PG::RI ? c + (size_t)j * R + 32 * p.i : r + (size_t)j * P + 32 * (p.i - PG::RI);
+    v[u] = j >= 0 ? *reinterpret_cast<const uint4*>(src + 8 * p.q) : make_uint4(0u, 0u, 0u, 0u);
+  }
+#pragma unroll
+  for (int u = 0; u < kItems; ++u) {
+    Piece p = piece(tid + u * kThreads);           // p.i is the same for a wave
+    if (p.i >= PG::KI) continue;
+    const bool there = s_src[p.t] >= 0;
+    if (p.i >= PG::RI) {
+      p.i -= PG::RI;
+      if (there) *reinterpret_cast<uint4*>(rope + chunk_of(p) * 16) = v[u];
+    } else if (st == kHi) {
+      if (there) *reinterpret_cast<uint4*>(pg + chunk_of(p) * 16) = v[u];
+    } else {
+      uint16_t sbits;
+      const uint32_t w = low_word(v[u], sbits);
+      const int g = 16 * p.i + p.t;
+      if (there) *reinterpret_cast<uint32_t*>(pg + g * 16 + 4 * p.q) = w;
+      if (there && p.q == 0) *reinterpret_cast<uint16_t*>(pg + PG::kScales + 2 * g) = sbits;
     }
-    for (int x = tid; x < PG::kRopeChunks; x += kThreads) rope_chunk(x, pg + 1024 * PG::RI);
-    return;
   }
-  uint8_t* pg = cv.lo_pool + (size_t)page * PG::kLoBytes;
-  for (int x = tid; x < PG::kGroups; x += kThreads) {
-    const int j = s_src[x & 15];
-    if (j < 0) continue;
-    const uint4* src = reinterpret_cast<const uint4*>(c + (size_t)j * R + 32 * (x >> 4));
-    const uint4 v[4] = {src[0], src[1], src[2], src[3]};
-    uint16_t sbits;
-    *reinterpret_cast<uint4*>(pg + x * 16) = low_group(v, sbits);
-    *reinterpret_cast<uint16_t*>(pg + PG::kScales + 2 * x) = sbits;
-  }
-  for (int x = tid; x < PG::kRopeChunks; x += kThreads) rope_chunk(x, pg + PG::kRopeAt);
 }
 
 // One token per sequence: thread 0 of the block decides and slots it, the
@@ -165,46 +170,50 @@ __global__ __launch_bounds__(128) void latent_step_kernel(AppendArgs a) {
   __syncthreads();
   if (s_code < 0) return;
   const int t = (s_code & 0x3FFFFFFF) % kPage, i = tid >> 2, q = tid & 3;
-  const int at = 64 * i + 16 * q + latent_swap(q, t);          // the piece's chunk in a HIGH page
+  const int at = chunk_of(Piece{i, q, t});
   if ((s_code >> 30) == kHi) {
     if (tid < kChunks)
       *reinterpret_cast<uint4*>(cv.hi_pool + (size_t)s_page * PG::kHiBytes + at * 16) = mine;
     return;
   }
   uint8_t* pg = cv.lo_pool + (size_t)s_page * PG::kLoBytes;
-  if (tid < PG::RI) {                                          // a 32-element group per thread
-    const uint4* src = reinterpret_cast<const uint4*>(c) + 4 * tid;
-    const uint4 v[4] = {src[0], src[1], src[2], src[3]};
-    uint16_t sbits;
-    *reinterpret_cast<uint4*>(pg + (16 * tid + t) * 16) = low_group(v, sbits);
-    *reinterpret_cast<uint16_t*>(pg + PG::kScales + 2 * (16 * tid + t)) = sbits;
+  uint16_t sbits;
+  const uint32_t w = low_word(mine, sbits);
+  if (tid < 4 * PG::RI) {
+    const int g = 16 * i + t;
+    *reinterpret_cast<uint32_t*>(pg + g * 16 + 4 * q) = w;
+    if (q == 0) *reinterpret_cast<uint16_t*>(pg + PG::kScales + 2 * g) = sbits;
+  } else if (tid < kChunks) {
+    *reinterpret_cast<uint4*>(pg + PG::kRopeAt + (at - 64 * PG::RI) * 16) = mine;
   }
-  if (tid >= 4 * PG::RI && tid < kChunks) *reinterpret_cast<uint4*>(pg + PG::kRopeAt + (at - 64 * PG::RI) * 16) = mine;
 }
 
-// Entries of list[0..n) below x (the list ascends).
-__device__ __forceinline__ int entries_below(const int32_t* list, int n, int x) {
-  int lo = 0, hi = n;
+// Entries of an ascending list below x, known to be lo or more and hi or fewer:
+// 16 lanes of a wave together, 16 entries at a time.
+__device__ __forceinline__ int entries_below(const int32_t* list, int lo, int hi, int x) {
+  const int lane = (int)threadIdx.x & 63, l = lane & 15;
   while (lo < hi) {
-    const int m = (lo + hi) >> 1;
-    if (list[m] < x) lo = m + 1;
-    else hi = m;
+    const int step = (hi - lo + 15) >> 4, at = lo + (l + 1) * step - 1;
+    const bool below = at < hi && list[at] < x;
+    const int c = __popc((uint32_t)(__ballot(below) >> (lane & 48)) & 0xFFFFu);
+    lo = min(lo + c * step, hi);
+    hi = min(lo + step - 1, hi);
   }
   return lo;
 }
 
 // Block (x, b) takes pages x, x + gridDim.x, ... of sequence b, HIGH's first.
 // A slot's row is cu[b] + its slot + the entries of the other store at lower
-// positions.
+// positions: of the position's predecessors those that are neither in this
+// store nor kept nowhere, so between position - slot - (positions not kept)
+// and position - slot, found among these.  A page's bytes are loaded first.
 template <int R, int P>
 __global__ __launch_bounds__(kThreads) void latent_read_kernel(LatentReadArgs a) {
   using PG = LatentPage<R, P>;
-  __shared__ int s_cu;
-  __shared__ int s_row[kPage];
+  __shared__ int s_cu[kWaves];
+  __shared__ int s_row[2][kPage];
   const CacheView& cv = a.cv;
   const int b = blockIdx.y, tid = (int)threadIdx.x;
-  if (tid == 0) s_cu = 0;
-  __syncthreads();
   int before = 0;
   for (int x = tid; x < b; x += kThreads) {
     const int32_t* o = counters_of(cv, x, a.layer);
@@ -212,62 +221,68 @@ __global__ __launch_bounds__(kThreads) void latent_read_kernel(LatentReadArgs a)
   }
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) before += __shfl_xor(before, off);
-  if ((tid & 63) == 0 && before) atomicAdd(&s_cu, before);
-  __syncthreads();
+  if ((tid & 63) == 0) s_cu[tid >> 6] = before;
   const int32_t* cnt = counters_of(cv, b, a.layer);
   const int n[2] = {cnt[kCntHi], cnt[kCntLo]};
-  const int cu = s_cu;
+  const int gone = cnt[kCntPos] - n[0] - n[1];     // positions not kept
+  __syncthreads();
+  int cu = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) cu += s_cu[w];
   if (blockIdx.x == 0 && tid == 0) {
     if (b == 0) a.cu[0] = 0;
     a.cu[b + 1] = cu + n[0] + n[1];
   }
   const int np_hi = (n[0] + kPage - 1) / kPage, np = np_hi + (n[1] + kPage - 1) / kPage;
-  for (int k = blockIdx.x; k < np; k += gridDim.x) {
+  int turn = 0;
+  for (int k = blockIdx.x; k < np; k += gridDim.x, turn ^= 1) {
     const int st = k < np_hi ? kHi : kLo, pidx = st == kHi ? k : k - np_hi;
     const int m = min(kPage, n[st] - pidx * kPage);
     const int page = block_table_of(cv, b, a.layer, st)[pidx];
-    __syncthreads();                               // the rows of the page before are used
-    if (tid < kPage) {
-      int row = -1;
-      if (tid < m) {
-        const int slot = pidx * kPage + tid;
-        const int pos = index_list_of(cv, b, a.layer, st)[slot];
-        row = cu + slot + entries_below(index_list_of(cv, b, a.layer, 1 - st), n[1 - st], pos);
-        if (row >= a.rows) row = -1;
-        else if (a.pos) a.pos[row] = pos;
+    const int slot = pidx * kPage + (tid >> 4);    // 16 lanes for each
+    const int pos = tid >> 4 < m ? index_list_of(cv, b, a.layer, st)[slot] : 0;
+    const uint8_t* pg =
+        st == kHi ? cv.hi_pool + (size_t)page * PG::kHiBytes : cv.lo_pool + (size_t)page * PG::kLoBytes;
+    const uint8_t* rope = pg + (st == kHi ? 1024 * PG::RI : PG::kRopeAt);
+    constexpr int kItems = (PG::KI + kWaves - 1) / kWaves;
+    uint4 v[kItems];
+    uint16_t s[kItems];
+#pragma unroll
+    for (int u = 0; u < kItems; ++u) {
+      Piece p = piece(tid + u * kThreads);         // p.i is the same for a wave
+      if (p.i >= PG::KI) continue;
+      if (p.i >= PG::RI) {
+        p.i -= PG::RI;
+        v[u] = *reinterpret_cast<const uint4*>(rope + chunk_of(p) * 16);
+      } else if (st == kHi) {
+        v[u] = *reinterpret_cast<const uint4*>(pg + chunk_of(p) * 16);
+      } else {
+        const int g = 16 * p.i + p.t;
+        v[u].x = *reinterpret_cast<const uint32_t*>(pg + g * 16 + 4 * p.q);
+        s[u] = *reinterpret_cast<const uint16_t*>(pg + PG::kScales + 2 * g);
       }
-      s_row[tid] = row;
     }
-    __syncthreads();
-    auto rope_chunk = [&](int x, const uint8_t* src) {
-      const int q = (x >> 4) & 3, row = s_row[latent_swap(q, x & 15)];
-      if (row >= 0)
-        *reinterpret_cast<uint4*>(a.r + (size_t)row * P + 32 * (x >> 6) + 8 * q) =
-            *reinterpret_cast<const uint4*>(src + x * 16);
-    };
-    if (st == kHi) {
-      const uint8_t* pg = cv.hi_pool + (size_t)page * PG::kHiBytes;
-      for (int x = tid; x < 64 * PG::RI; x += kThreads) {
-        const int q = (x >> 4) & 3, row = s_row[latent_swap(q, x & 15)];
-        if (row >= 0)
-          *reinterpret_cast<uint4*>(a.c + (size_t)row * R + 32 * (x >> 6) + 8 * q) =
-              *reinterpret_cast<const uint4*>(pg + x * 16);
-      }
-      for (int x = tid; x < PG::kRopeChunks; x += kThreads) rope_chunk(x, pg + 1024 * PG::RI);
-    } else {
-      const uint8_t* pg = cv.lo_pool + (size_t)page * PG::kLoBytes;
-      for (int x = tid; x < PG::kGroups; x += kThreads) {
-        const int row = s_row[x & 15];
-        if (row < 0) continue;
-        const uint4 w = *reinterpret_cast<const uint4*>(pg + x * 16);
-        const float s = half_value(*reinterpret_cast<const uint16_t*>(pg + PG::kScales + 2 * x));
-        uint4* dst = reinterpret_cast<uint4*>(a.c + (size_t)row * R + 32 * (x >> 4));
-        dst[0] = low_values(w.x, s);
-        dst[1] = low_values(w.y, s);
-        dst[2] = low_values(w.z, s);
-        dst[3] = low_values(w.w, s);
-      }
-      for (int x = tid; x < PG::kRopeChunks; x += kThreads) rope_chunk(x, pg + PG::kRopeAt);
+    int row = -1;
+    if (tid >> 4 < m) {
+      const int most = pos - slot;
+      row = cu + slot + entries_below(index_list_of(cv, b, a.layer, 1 - st), max(0, most - gone),
+                                      min(n[1 - st], most), pos);
+      if (row >= a.rows) row = -1;
+    }
+    if ((tid & 15) == 0) {
+      s_row[turn][tid >> 4] = row;
+      if (row >= 0 && a.pos) a.pos[row] = pos;
+    }
+    __syncthreads();                               // this turn's rows; the ones before last have been used
+#pragma unroll
+    for (int u = 0; u < kItems; ++u) {
+      const Piece p = piece(tid + u * kThreads);
+      if (p.i >= PG::KI) continue;
+      const int to = s_row[turn][p.t];
+      const bool latent = p.i < PG::RI;
+      uint16_t* dst = latent ? a.c + (size_t)to * R + 32 * p.i : a.r + (size_t)to * P + 32 * (p.i - PG::RI);
+      const uint4 x = latent && st == kLo ? low_values(v[u].x, half_value(s[u])) : v[u];
+      if (to >= 0) *reinterpret_cast<uint4*>(dst + 8 * p.q) = x;
     }
   }
 }
