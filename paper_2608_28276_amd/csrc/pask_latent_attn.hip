@@ -360,6 +360,7 @@ __global__ __launch_bounds__(64 * latent_waves(NHT), 2) void latent_attn_kernel(
     const float base = mx == -INFINITY ? 0.0f : mx;
     float w[4 * JP];
     part = 0.0f;
+    const uint32_t p_at = lds_address(sm.p) + (ht * 64 + fresh(lane)) * 16 + page0 * 8;
 #pragma unroll
     for (int r = 0; r < 4 * JP; ++r) {
       w[r] = __builtin_amdgcn_exp2f(x[r] - base);
@@ -367,7 +368,7 @@ __global__ __launch_bounds__(64 * latent_waves(NHT), 2) void latent_attn_kernel(
     }
 #pragma unroll
     for (int jp = 0; jp < JP; ++jp)
-      write_lds8(lds_address(sm.p) + (ht * 64 + lane) * 16 + (page0 + jp) * 8,
+      write_lds8(p_at + jp * 8,
                  make_uint2(pack_bf16x2(w[4 * jp], w[4 * jp + 1]), pack_bf16x2(w[4 * jp + 2], w[4 * jp + 3])));
   };
   // Scores and weights of a tile in LDS; true for every wave if some head's
@@ -385,11 +386,12 @@ __global__ __launch_bounds__(64 * latent_waves(NHT), 2) void latent_attn_kernel(
       // operands of kAhead steps read in advance: in pinned order, as left to
       // itself the compiler saves registers and waits for every read.
       constexpr int kAhead = JP == 1 ? 6 : (NHT >= 8 ? 2 : 3);
-      const uint32_t kb = fresh(lds_address(tile) + k_at);
+      // Addresses are formed here: kept in registers, they would push others out.
+      const uint32_t kb = lds_address(tile) + fresh(k_at), qb = fresh(q_at);
       auto operand = [&](int i, int jp) { return read_lds16(kb + jp * PG::kHiBytes + i * 1024); };
       f32x4_t s[2] = {f32x4_t{0.0f, 0.0f, 0.0f, 0.0f}, f32x4_t{0.0f, 0.0f, 0.0f, 0.0f}};
       // Steps whose queries are in LDS come last.
-      auto queries = [&](int i) { return i < KI - kQl ? qf[i] : read_lds16(q_at + (i - KI + kQl) * 1024); };
+      auto queries = [&](int i) { return i < KI - kQl ? qf[i] : read_lds16(qb + (i - KI + kQl) * 1024); };
       uint4 kf[kAhead][JP], ql[2];
 #pragma unroll
       for (int i = 0; i < kAhead; ++i)
@@ -409,10 +411,10 @@ __global__ __launch_bounds__(64 * latent_waves(NHT), 2) void latent_attn_kernel(
       }
       if constexpr (JP == 1) s[0] += s[1];
       top = -INFINITY;
+      const int left = m - page0 * kPage - 4 * (fresh(lane) >> 4);
 #pragma unroll
       for (int r = 0; r < 4 * JP; ++r) {
-        const int slot = (page0 + (r >> 2)) * kPage + 4 * q4 + (r & 3);
-        x[r] = slot < m ? s[r >> 2][r & 3] * a.scale_log2 : -INFINITY;
+        x[r] = (r >> 2) * kPage + (r & 3) < left ? s[r >> 2][r & 3] * a.scale_log2 : -INFINITY;
         top = fmaxf(top, x[r]);
       }
       weigh();
@@ -450,7 +452,7 @@ __global__ __launch_bounds__(64 * latent_waves(NHT), 2) void latent_attn_kernel(
     }
   };
   auto add_values = [&](const uint8_t* tile) {
-    const uint32_t vs = lds_address(tile) + v_at, ps = lds_address(sm.p) + lane * 16;
+    const uint32_t vs = lds_address(tile) + fresh(v_at), ps = lds_address(sm.p) + fresh(lane) * 16;
     constexpr int kW = NHT < 4 ? NHT : 4;          // weights read in advance
     uint4 w[kW], v[DT > 4 ? 8 : 4];
 #pragma unroll
