@@ -164,33 +164,22 @@ struct Tile {
   static constexpr int kBytes = 2 * PG::kHiBytes, kRaw = kBytes - 2 * PG::kLoBytes;
   static constexpr int kLoChunks = PG::kLoBytes / 16;
 
-  // p0, p1: the two pages (p1 negative: none).  The waves share the 1 KiB pieces.
-  __device__ __forceinline__ static void copy_high(const uint8_t* pool, int p0, int p1, uint8_t* tile, int wave,
-                                                   int lane) {
-    lane = fresh(lane);
-    const uint8_t* b0 = pool + (size_t)p0 * PG::kHiBytes + lane * 16;
-    if (p1 >= 0) {
-      const uint8_t* b1 = pool + (size_t)p1 * PG::kHiBytes - PG::kHiBytes + lane * 16;
-#pragma unroll
-      for (int k = 0; k < (2 * PG::KI + kWaves - 1) / kWaves; ++k) {
-        const int x = wave + k * kWaves;
-        if ((k + 1) * kWaves <= 2 * PG::KI || x < 2 * PG::KI)
-          load_to_lds<true>((x < PG::KI ? b0 : b1) + x * 1024, tile + x * 1024);
-      }
-    } else {
-      for (int x = wave; x < PG::KI; x += kWaves) load_to_lds<true>(b0 + x * 1024, tile + x * 1024);
-    }
+  // The copy of a tile's pages, in pieces of 64 chunks (1 KiB).
+  struct Copy {
+    const uint8_t *b0, *b1;                        // chunk c of the two pages: at (c < split ? b0 : b1) + 16 c
+    int split, chunks;
+    uint8_t* to;
+  };
+  __device__ __forceinline__ static Copy no_copy() { return Copy{nullptr, nullptr, 0, 0, nullptr}; }
+  __device__ __forceinline__ static Copy copy_of(const CacheView& cv, const Item& x, uint8_t* tile) {
+    const uint8_t* pool = x.high() ? cv.hi_pool : cv.lo_pool;
+    const int n = x.high() ? PG::kHiChunks : kLoChunks;
+    return Copy{pool + (size_t)x.p0 * (16 * n), pool + ((long long)x.p1 - 1) * (16 * n), n,
+                x.slots() == 0 ? 0 : x.p1 < 0 ? n : 2 * n, tile + (x.high() ? 0 : kRaw)};
   }
-  __device__ __forceinline__ static void copy_low(const uint8_t* pool, int p0, int p1, uint8_t* tile, int wave, int lane) {
-    lane = fresh(lane);
-    const uint8_t* b0 = pool + (size_t)p0 * PG::kLoBytes;
-    const uint8_t* b1 = pool + (size_t)(p1 < 0 ? p0 : p1) * PG::kLoBytes - PG::kLoBytes;
-#pragma unroll
-    for (int k = 0; k < (2 * kLoChunks + T - 1) / T; ++k) {
-      const int c = (wave + k * kWaves) * 64 + lane;
-      if (c < 2 * kLoChunks)
-        load_to_lds<true>((c < kLoChunks ? b0 : b1) + c * 16, tile + kRaw + (wave + k * kWaves) * 1024);
-    }
+  __device__ __forceinline__ static void copy_piece(const Copy& y, int piece) {
+    const int c = piece * 64 + (fresh((int)threadIdx.x) & 63);
+    if (c < y.chunks) load_to_lds<true>((c < y.split ? y.b0 : y.b1) + c * 16, y.to + piece * 1024);
   }
   // Slots from n on as zeros: what lies there is not an entry (any bytes, NaN
   // among them), and a weight of 0 does not make a NaN value harmless.
@@ -325,12 +314,19 @@ __global__ __launch_bounds__(64 * latent_waves(NHT), 2) void latent_attn_kernel(
     return Item{uni((int)x.x), uni((int)x.y), uni((int)x.z), uni((int)x.w)};
   };
   using TL = Tile<R, P, T>;
+  // With two tiles under way the copy of a tile is issued piece by piece,
+  // between the score steps: at once, each wave waited about 900 cycles for room
+  // in the queue (128 heads: 288 us, 250 so).  With one under way it is issued
+  // at once: the sooner the better (16 heads, 64 sequences: 53 us, 56 between
+  // the steps).
+  constexpr bool kBetween = D == 2;
+  static_assert(!kBetween || QW == NW, "every wave scores");
+  constexpr int NP = (2 * KI + NW - 1) / NW;       // pieces of a wave
   bool long_wait = true;                           // the newest copies are not a full HIGH tile's
+  typename TL::Copy copy = TL::no_copy();
+  auto issue = [&](int k) { TL::copy_piece(copy, wave + k * NW); };
   auto fetch = [&](const Item& x, uint8_t* tile) {
-    if (x.slots() > 0) {
-      if (x.high()) TL::copy_high(cv.hi_pool, x.p0, x.p1, tile, wave, lane);
-      else TL::copy_low(cv.lo_pool, x.p0, x.p1, tile, wave, lane);
-    }
+    copy = TL::copy_of(cv, x, tile);
     long_wait = !x.high() || x.p1 < 0;
   };
   uint4 qf[KI - kQl];
@@ -371,7 +367,7 @@ __global__ __launch_bounds__(64 * latent_waves(NHT), 2) void latent_attn_kernel(
       write_lds8(p_at + jp * 8,
                  make_uint2(pack_bf16x2(w[4 * jp], w[4 * jp + 1]), pack_bf16x2(w[4 * jp + 2], w[4 * jp + 3])));
   };
-  // Scores and weights of a tile in LDS; true for every wave if some head's
+  // Scores and weights of a tile in LDS, and the copies of the tile ahead; true for every wave if some head's
   // reference has to move first (move_reference).
   auto score = [&](const Item& at, uint8_t* tile) {
     const int m = at.slots();
@@ -407,6 +403,7 @@ __global__ __launch_bounds__(64 * latent_waves(NHT), 2) void latent_attn_kernel(
           if (i + kAhead < KI) kf[i % kAhead][jp] = operand(i + kAhead, jp);
         }
         if (kQl > 0 && i + 2 >= KI - kQl && i + 2 < KI) ql[i & 1] = queries(i + 2);
+        if (kBetween && i * NP / KI != (i + 1) * NP / KI) issue(i * NP / KI);
         __builtin_amdgcn_sched_barrier(0);
       }
       if constexpr (JP == 1) s[0] += s[1];
@@ -484,14 +481,22 @@ __global__ __launch_bounds__(64 * latent_waves(NHT), 2) void latent_attn_kernel(
   restart();
 #pragma unroll
   for (int k = 0; k < D; ++k)
-    if (u + k < u1) fetch(item(u + k), buffer(k));
+    if (u + k < u1) {
+      fetch(item(u + k), buffer(k));
+      for (int j = 0; j < NP; ++j) issue(j);
+    }
   wait_loads();
   __syncthreads();
-  // With every wave done with the tile before: a tile on its way into its buffer.
+  // With every wave done with the tile before: the tile that goes into its buffer.
   auto look_ahead = [&]() {
+    copy = TL::no_copy();
     if (u + D >= u1) return;
     if (((u + D - u0) & 63) == 0) fill(u + D);
     fetch(item(u + D), buffer(D));
+    if (!kBetween) {
+#pragma unroll
+      for (int k = 0; k < NP; ++k) issue(k);
+    }
   };
   auto advance = [&]() {
     ++u;
@@ -595,59 +600,86 @@ __global__ __launch_bounds__(64 * latent_waves(NHT), 2) void latent_attn_kernel(
 // ---------------------------------------------------------------------------
 // The partials of a head: maxima and sums give each one's weight, then the
 // weighted values are added in order of the partials (slot of the first, then
-// the first slots of the workers after it).  Few partials: a wave per head.
-// Many: a workgroup per head, its waves taking every fourth partial and adding
-// up through LDS.
+// the first slots of the workers after it).  Up to 8 partials: a wave per head.
+// More: a workgroup per slice of a head, R / (8 slices) lanes to a partial, as
+// many partials at a time as fit, added up through LDS.  With few heads in the
+// call a head is cut into slices, down to 64 elements (275 partials of 20 heads:
+// 12 us whole, 6.7 in 8 slices); with enough to fill the chip it is not (64
+// sequences of 16 heads: 6.6 us whole, 12 in slices, each of which finds the
+// maximum again).
 template <int R>
-__global__ __launch_bounds__(kThreads) void latent_merge_kernel(LatentAttnArgs a, int tile_heads) {
-  constexpr int E = R / 64;                        // elements per lane
-  __shared__ float s_o[kWaves][R], s_w[kWaves];
+__global__ __launch_bounds__(kThreads) void latent_merge_kernel(LatentAttnArgs a, int tile_heads, int log_slices) {
+  constexpr int E = R / 64;                        // elements per lane of a wave's head
+  __shared__ f32x4_t s_o[2][kThreads];
+  __shared__ float s_w[kThreads / 8];
   const int b = blockIdx.y, lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
   const int first = a.ws_seq[2 * b], n = a.ws_seq[2 * b + 1];
   if (n == 0) return;
-  const bool shared = n > 8;                       // by all waves of the workgroup
   auto slot = [&](int k) { return k == 0 ? first : 2 * (first / 2 + k); };
-  const int step = shared ? (int)gridDim.x : (int)gridDim.x * kWaves;
-  for (int h0 = shared ? (int)blockIdx.x : (int)blockIdx.x * kWaves; h0 < a.heads; h0 += step) {
-    const int h = shared ? h0 : h0 + wave;
-    if (h >= a.heads) continue;                    // only of a wave with a head of its own
+  auto maxima = [&](int h) {
     float top = -INFINITY;
     for (int k = lane; k < n; k += 64) top = fmaxf(top, a.ws_ml[((size_t)slot(k) * tile_heads + h) * 2]);
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
-    const float base = top == -INFINITY ? 0.0f : top;
-    float o[E] = {}, total = 0.0f;
-    const int k0 = shared ? wave : 0, dk = shared ? kWaves : 1;
+    return top;
+  };
+  if (n <= 8) {
+    for (int h = (int)blockIdx.x * kWaves + wave; h < a.heads; h += (int)gridDim.x * kWaves) {
+      const float top = maxima(h), base = top == -INFINITY ? 0.0f : top;
+      float o[E] = {}, total = 0.0f;
 #pragma unroll 4
-    for (int k = k0; k < n; k += dk) {
+      for (int k = 0; k < n; ++k) {
+        const size_t at = (size_t)slot(k) * tile_heads + h;
+        const float2 ml = *reinterpret_cast<const float2*>(a.ws_ml + at * 2);
+        const float* src = a.ws_o + at * R + lane * E;
+        const float w = __builtin_amdgcn_exp2f(ml.x - base);
+        total += w * ml.y;
+#pragma unroll
+        for (int u = 0; u < E; ++u) o[u] += w * src[u];
+      }
+      const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+      const size_t at = (size_t)b * a.heads + h;
+      uint32_t* dst = reinterpret_cast<uint32_t*>(a.out + at * R + lane * E);
+#pragma unroll
+      for (int u = 0; u < E / 2; ++u) dst[u] = pack_bf16x2(o[2 * u] * inv, o[2 * u + 1] * inv);
+      if (lane == 0 && a.lse) a.lse[at] = total == 0.0f ? -INFINITY : (base + __builtin_amdgcn_logf(total)) * kLn2;
+    }
+    return;
+  }
+  const int lanes = (R / 8) >> log_slices, groups = kThreads / lanes;
+  const int g = (int)threadIdx.x / lanes, l = (int)threadIdx.x - g * lanes;
+  for (int x = blockIdx.x; x < a.heads << log_slices; x += gridDim.x) {
+    const int h = x >> log_slices, part = x - (h << log_slices), e = (part * lanes + l) * 8;
+    const float top = maxima(h), base = top == -INFINITY ? 0.0f : top;
+    f32x4_t o[2] = {f32x4_t{0.0f, 0.0f, 0.0f, 0.0f}, f32x4_t{0.0f, 0.0f, 0.0f, 0.0f}};
+    float total = 0.0f;
+#pragma unroll 4
+    for (int k = g; k < n; k += groups) {
       const size_t at = (size_t)slot(k) * tile_heads + h;
       const float2 ml = *reinterpret_cast<const float2*>(a.ws_ml + at * 2);
-      const float* src = a.ws_o + at * R + lane * E;
+      const f32x4_t* v = reinterpret_cast<const f32x4_t*>(a.ws_o + at * R + e);
       const float w = __builtin_amdgcn_exp2f(ml.x - base);
       total += w * ml.y;
-#pragma unroll
-      for (int u = 0; u < E; ++u) o[u] += w * src[u];
+      o[0] += v[0] * w;
+      o[1] += v[1] * w;
     }
-    if (shared) {
-      __syncthreads();                             // the head before has been read
-#pragma unroll
-      for (int u = 0; u < E; ++u) s_o[wave][lane * E + u] = o[u];
-      if (lane == 0) s_w[wave] = total;
-      __syncthreads();
-      if (wave > 0) continue;
-#pragma unroll
-      for (int w = 1; w < kWaves; ++w) {
-        total += s_w[w];
-#pragma unroll
-        for (int u = 0; u < E; ++u) o[u] += s_o[w][lane * E + u];
-      }
+    __syncthreads();                               // the sums before have been read
+    s_o[0][threadIdx.x] = o[0];
+    s_o[1][threadIdx.x] = o[1];
+    if (l == 0) s_w[g] = total;
+    __syncthreads();
+    if (g > 0) continue;
+    for (int i = 1; i < groups; ++i) {
+      o[0] += s_o[0][i * lanes + l];
+      o[1] += s_o[1][i * lanes + l];
+      total += s_w[i];
     }
     const float inv = total == 0.0f ? 0.0f : 1.0f / total;
     const size_t at = (size_t)b * a.heads + h;
-    uint32_t* dst = reinterpret_cast<uint32_t*>(a.out + at * R + lane * E);
-#pragma unroll
-    for (int u = 0; u < E / 2; ++u) dst[u] = pack_bf16x2(o[2 * u] * inv, o[2 * u + 1] * inv);
-    if (lane == 0 && a.lse) a.lse[at] = total == 0.0f ? -INFINITY : (base + __builtin_amdgcn_logf(total)) * kLn2;
+    *reinterpret_cast<uint4*>(a.out + at * R + e) =
+        make_uint4(pack_bf16x2(o[0][0] * inv, o[0][1] * inv), pack_bf16x2(o[0][2] * inv, o[0][3] * inv),
+                   pack_bf16x2(o[1][0] * inv, o[1][1] * inv), pack_bf16x2(o[1][2] * inv, o[1][3] * inv));
+    if (e == 0 && a.lse) a.lse[at] = total == 0.0f ? -INFINITY : (base + __builtin_amdgcn_logf(total)) * kLn2;
   }
 }
 
@@ -685,10 +717,13 @@ hipError_t launch_latent_attention(const LatentAttnArgs& a, hipStream_t s) {
   if (e != hipSuccess) return e;
   if (a.workers == 1) return hipSuccess;           // nothing is shared
   const int heads = 16 * latent_head_tiles(a.heads);
-  const dim3 grid(std::max(1, std::min(a.heads, 1024 / a.batch)), a.batch);
-  if (a.rank == 128) latent_merge_kernel<128><<<grid, dim3(kThreads), 0, s>>>(a, heads);
-  else if (a.rank == 256) latent_merge_kernel<256><<<grid, dim3(kThreads), 0, s>>>(a, heads);
-  else latent_merge_kernel<512><<<grid, dim3(kThreads), 0, s>>>(a, heads);
+  constexpr int kBlocks = 1024;
+  int log_slices = 0;
+  while ((a.rank / 64) >> (log_slices + 1) && ((int64_t)a.batch * a.heads << (log_slices + 1)) <= kBlocks) ++log_slices;
+  const dim3 grid(std::max(1, std::min(a.heads << log_slices, kBlocks / a.batch)), a.batch);
+  if (a.rank == 128) latent_merge_kernel<128><<<grid, dim3(kThreads), 0, s>>>(a, heads, log_slices);
+  else if (a.rank == 256) latent_merge_kernel<256><<<grid, dim3(kThreads), 0, s>>>(a, heads, log_slices);
+  else latent_merge_kernel<512><<<grid, dim3(kThreads), 0, s>>>(a, heads, log_slices);
   return hipGetLastError();
 }
 
