@@ -83,7 +83,7 @@ int debug_check(const char* where, hipError_t e, const pask_latent_cache* cache,
 int workers_for(const pask_latent_geom& g, int32_t batch, int32_t max_ctx_hint) {
   const int64_t hint = max_ctx_hint < 1 ? g.max_tokens_per_seq : std::min(max_ctx_hint, g.max_tokens_per_seq);
   // both stores of a sequence may end in a part of a tile
-  return pask::latent_workers(g.rank, g.rope_dim, g.n_q_heads, batch * ((hint + kTileSlots - 1) / kTileSlots + 1));
+  return pask::latent_workers(g.n_q_heads, batch * ((hint + kTileSlots - 1) / kTileSlots + 1));
 }
 
 // Two partial results per workgroup (its first sequence and its last), and two

@@ -93,11 +93,14 @@ __device__ __forceinline__ ListPlace find_in_list(const LatentAttnArgs& a, long 
 }
 
 // Tiles each worker takes.  More workers finish their tiles sooner but leave
-// more partial results, whose writing and merging costs about 1/40 of a tile's
-// time for 16 heads when the whole chip shares it: W tiles / u + W NHT / 40 is
-// least at W = sqrt(40 tiles / NHT) tiles' times.
+// more partial results, whose writing and merging costs about 1/150 of a tile's
+// time for 16 heads when the whole chip shares it: with W workers the tiles take
+// total / W tiles' times and the partials W head_tiles / 150, least at
+// W = sqrt(150 total / head_tiles).  Rank 512, this rule / all workers / 1/76:
+// one sequence of 8,000 tokens, 64 heads 28.6 / 41.5 / 29.3 us; four of 16,000,
+// 128 heads 66.3 / 76.7 / 86.6; one of 64,001, 128 heads 69.5 / 66.7 / 81.7.
 __device__ __forceinline__ long long tiles_per_worker(long long total, int workers, int head_tiles) {
-  const int best = (int)sqrtf(76.0f * (float)total / (float)head_tiles) + 1;
+  const int best = (int)sqrtf(150.0f * (float)total / (float)head_tiles) + 1;
   const int n = min(workers, best);
   return (total + n - 1) / n;
 }
@@ -696,9 +699,7 @@ void launch_heads(const LatentAttnArgs& a, hipStream_t s) {
 
 }  // namespace
 
-int latent_workers(int rank, int rope, int heads, int64_t tiles) {
-  (void)rank;
-  (void)rope;
+int latent_workers(int heads, int64_t tiles) {
   const int resident = latent_head_tiles(heads) >= 4 ? 256 : 512;
   return (int)std::max<int64_t>(1, std::min<int64_t>(resident, tiles));
 }

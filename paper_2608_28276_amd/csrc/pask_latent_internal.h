@@ -48,7 +48,7 @@ struct LatentPromptArgs {
 // Head tiles (16 heads) the decode kernel is built for: 1, 2, 4 or 8.
 inline int latent_head_tiles(int heads) { return heads <= 16 ? 1 : heads <= 32 ? 2 : heads <= 64 ? 4 : 8; }
 // Workgroups of the decode kernel; at most `tiles` (of 32 slots, and one per sequence).
-int latent_workers(int rank, int rope, int heads, int64_t tiles);
+int latent_workers(int heads, int64_t tiles);
 
 hipError_t launch_latent_append(const LatentAppendArgs& a, hipStream_t s);   // chooses the one-token kernel
 hipError_t launch_latent_read(const LatentReadArgs& a, hipStream_t s);

@@ -98,11 +98,31 @@ __global__ __launch_bounds__(64 * W, 2) void latent_prompt_kernel(LatentPromptAr
   const int g = lane >> 5, n = lane & 31;
   // Workgroups go to the 8 XCDs in turn.  With a multiple of 8 heads each XCD gets neighbouring heads.
   int head = (int)blockIdx.x % a.heads;
-  const int rest = (int)blockIdx.x / a.heads;
+  int rest = (int)blockIdx.x / a.heads;
   if (a.heads % 8 == 0) head = head % 8 * (a.heads / 8) + head / 8;
-  const int b = rest % a.batch, tile = q_tiles - 1 - rest / a.batch;   // the longest first
-  const int q0 = min(max(a.cu_q[b], 0), a.total_q), q1 = min(max(a.cu_q[b + 1], 0), a.total_q);
-  const int k0 = min(max(a.cu_k[b], 0), a.total_k), k1 = min(max(a.cu_k[b + 1], 0), a.total_k);
+  auto q_at = [&](int b) { return min(max(a.cu_q[b], 0), a.total_q); };
+  auto k_at = [&](int b) { return min(max(a.cu_k[b], 0), a.total_k); };
+  // The longest tiles first: the last of every sequence before the ones before
+  // it, or by the keys they see where there are few enough to rank in a wave's
+  // lanes (with more the rest evens out; 8 chunks of 266-1,024 queries with up
+  // to 2,306 keys before them, 20 heads: 208 us by the first, 168 so).
+  const int items = q_tiles * a.batch;
+  if (items <= 64) {
+    const int b = lane % a.batch, tile = q_tiles - 1 - lane / a.batch;
+    int keys = -1;                                 // of lane's item; an empty tile is the last
+    if (lane < items) {
+      const int nq = min(q_at(b + 1) - q_at(b), a.max_q), last = min(tile * kRows + kRows, nq) - 1;
+      if (tile * kRows < nq) keys = max(0, k_at(b + 1) - k_at(b) - (q_at(b + 1) - q_at(b)) + last + 1);
+    }
+    int before = 0;
+    for (int y = 0; y < items; ++y) {
+      const int other = __builtin_amdgcn_readlane(keys, y);
+      before += other > keys || (other == keys && y < lane);
+    }
+    rest = __builtin_amdgcn_readfirstlane((int)__ffsll((unsigned long long)__ballot(lane < items && before == rest)) - 1);
+  }
+  const int b = rest % a.batch, tile = q_tiles - 1 - rest / a.batch;
+  const int q0 = q_at(b), q1 = q_at(b + 1), k0 = k_at(b), k1 = k_at(b + 1);
   const int nq = q1 - q0, nk = max(k1 - k0, 0), nq_in = min(nq, a.max_q);
   if (tile * kRows >= nq_in) return;
   const int row0 = tile * kRows + wave * 32, row = row0 + n;   // this lane's query
