@@ -146,7 +146,8 @@ size_t pask_latent_workspace_bytes(const pask_latent_geom* geom, int32_t batch, 
  * need workspaces of their own.
  *
  * Errors: PASK_E_ARG (null or misaligned pointers: q_dev, out_dev, c_new_dev,
- * r_new_dev 16 bytes, lse_dev 4; softmax_scale not finite), PASK_E_SHAPE,
+ * r_new_dev 16 bytes, lse_dev 4; softmax_scale, or its product with log2 e,
+ * not finite in fp32), PASK_E_SHAPE,
  * PASK_E_POLICY, PASK_E_UNSUPPORTED (policy with a recent window),
  * PASK_E_CAPACITY (workspace too small), PASK_E_HIP. */
 int pask_latent_decode_attn(const pask_policy* policy, pask_latent_cache* cache, int32_t layer, int32_t batch,
@@ -174,7 +175,8 @@ int pask_latent_decode_attn(const pask_policy* policy, pask_latent_cache* cache,
  * batch 1..65535.
  *
  * Errors: PASK_E_ARG (null or misaligned pointers: q_dev, kv_dev, r_dev,
- * out_dev 16 bytes, the others 4; a negative size; softmax_scale not finite),
+ * out_dev 16 bytes, the others 4; a negative size; softmax_scale, or its
+ * product with log2 e, not finite in fp32),
  * PASK_E_SHAPE (unsupported dimensions, or batch * n_heads *
  * ceil(max_q / (64 if max_q <= 64 else 256)) of 2^23 or more),
  * PASK_E_HIP.  With max_q or total_q 0 nothing is done; with total_k 0 the

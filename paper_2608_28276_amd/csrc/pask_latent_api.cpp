@@ -122,6 +122,10 @@ pask::LatentAppendArgs append_args(const pask_policy* policy, pask_latent_cache*
 
 bool rows_ok(const void* p) { return p && aligned(p, 16); }
 
+// The kernels' exponentials are in base 2.
+float scale_log2(float softmax_scale) { return (float)((double)softmax_scale * 1.4426950408889634); }
+bool scale_ok(float softmax_scale) { return isfinite(softmax_scale) && isfinite(scale_log2(softmax_scale)); }
+
 }  // namespace
 
 extern "C" {
@@ -214,7 +218,7 @@ int pask_latent_decode_attn(const pask_policy* policy, pask_latent_cache* cache,
   const pask_latent_geom& g = cache->geom;
   if (!rows_ok(q_dev) || !rows_ok(out_dev) || !aligned(lse_dev, 4)) return PASK_E_ARG;
   if (tags_new_dev && (!rows_ok(c_new_dev) || !rows_ok(r_new_dev))) return PASK_E_ARG;
-  if (!isfinite(softmax_scale)) return PASK_E_ARG;
+  if (!scale_ok(softmax_scale)) return PASK_E_ARG;
   const int workers = workers_for(g, batch, max_ctx_hint);
   const WsLayout w = ws_layout(g, batch, workers);
   if (!ws_dev || !aligned(ws_dev, 256)) return PASK_E_ARG;
@@ -233,7 +237,7 @@ int pask_latent_decode_attn(const pask_policy* policy, pask_latent_cache* cache,
   a.ws_o = reinterpret_cast<float*>(ws);
   a.ws_ml = reinterpret_cast<float*>(ws + w.ml_off);
   a.ws_seq = reinterpret_cast<int32_t*>(ws + w.seq_off);
-  a.scale_log2 = (float)((double)softmax_scale * 1.4426950408889634);
+  a.scale_log2 = scale_log2(softmax_scale);
   a.layer = layer;
   a.batch = batch;
   a.heads = g.n_q_heads;
@@ -250,7 +254,7 @@ int pask_latent_prompt_attn(int32_t batch, int32_t n_heads, int32_t nope_dim, in
   if (batch < 1 || batch > 65535 || n_heads < 1 || n_heads > PASK_LATENT_MAX_HEADS) return PASK_E_SHAPE;
   if ((nope_dim != 64 && nope_dim != 128) || (v_dim != 64 && v_dim != 128) || (rope_dim != 32 && rope_dim != 64))
     return PASK_E_SHAPE;
-  if (max_q < 0 || total_q < 0 || total_k < 0 || !isfinite(softmax_scale)) return PASK_E_ARG;
+  if (max_q < 0 || total_q < 0 || total_k < 0 || !scale_ok(softmax_scale)) return PASK_E_ARG;
   if (!cu_q_dev || !cu_k_dev || !aligned(cu_q_dev, 4) || !aligned(cu_k_dev, 4) || !aligned(lse_dev, 4))
     return PASK_E_ARG;
   if (max_q == 0 || total_q == 0) return PASK_OK;
@@ -264,7 +268,7 @@ int pask_latent_prompt_attn(int32_t batch, int32_t n_heads, int32_t nope_dim, in
   a.lse = lse_dev;
   a.cu_q = cu_q_dev;
   a.cu_k = cu_k_dev;
-  a.scale_log2 = (float)((double)softmax_scale * 1.4426950408889634);
+  a.scale_log2 = scale_log2(softmax_scale);
   a.batch = batch;
   a.heads = n_heads;
   a.nope = nope_dim;

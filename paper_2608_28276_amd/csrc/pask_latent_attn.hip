@@ -250,7 +250,7 @@ struct Tile {
 //           2^-8 of a weight; independent over slots, so it averages out below
 //           the output's own rounding); their sum is kept of the unrounded ones
 //           in fp32.  A head's reference moves only when a score exceeds it by
-//           more than kHeadroom: weights up to 2^60 are as precise as those
+//           more than kHeadroom: weights up to 2^16 are as precise as those
 //           below 1, and the sums of values, which fill the registers, are left
 //           alone in the loop.
 //   values  O^T += C^T P^T: wave w of W owns output elements [w R / W, (w + 1) R
@@ -264,7 +264,7 @@ struct Tile {
 // workgroup keeps two tiles under way.
 constexpr int latent_waves(int head_tiles) { return head_tiles >= 4 ? 8 : 4; }
 constexpr int latent_ahead(int head_tiles) { return head_tiles >= 4 ? 2 : 1; }
-constexpr float kHeadroom = 60.0f;
+constexpr float kHeadroom = 16.0f;
 
 template <int R, int P, int NHT>
 __global__ __launch_bounds__(64 * latent_waves(NHT), 2) void latent_attn_kernel(LatentAttnArgs a) {

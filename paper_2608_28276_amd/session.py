@@ -314,6 +314,8 @@ class PaskLatentSession:
             latent.check_tensor("tags_new", tags_new, torch.uint8, (b,), self.device)
             self._bf16("c_new", c_new, b, g.rank)
             self._bf16("r_new", r_new, b, g.rope_dim)
+        elif c_new is not None or r_new is not None:
+            raise pask.PaskError(pask.PASK_E_ARG, "decode: a new token without tags_new")
         self._call(latent.pask_latent_decode_attn, self.policy, self.cache, layer, b, q, out, lse, tags_new, c_new,
                    r_new, self.softmax_scale, max_ctx_hint or self.max_ctx_hint, self.ws, self.ws_bytes)
 

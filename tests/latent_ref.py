@@ -11,7 +11,10 @@ u32 = 2^-24:
            bf16, u16.
   outputs  |err| <= u16 |o| + (u16 + 2 delta + 2^-22 + n u32) sum p |v|
   lse      |err| <= delta + (n + 16) u32 + 4 u32 |lse|
-all times 1.05 for the second-order terms.
+all times 1.05 for the second-order terms.  Underflow adds 2^-126 (sum |v| + 1)
+to an output: an exponential below 2^-126 may be taken as 0, the largest score's
+is 1 or more (no reference lies above it), so after the division an entry's
+weight lacks 2^-126 at most; and a result below 2^-126 may be taken as 0 itself.
 """
 
 from __future__ import annotations
@@ -100,6 +103,7 @@ def attention(q, keys, values, scale, seen=None):
     lse = np.where(some, top + np.log(np.where(some, total, 1.0)), -np.inf)
     mass = p @ np.abs(values)
     out_tol = 1.05 * (U16 * np.abs(out) + (U16 + 2 * delta + 2.0 ** -22 + n * U32)[:, None] * mass)
+    out_tol += 2.0 ** -126 * (seen @ np.abs(values) + 1.0)
     lse_tol = 1.05 * (delta + (n + 16) * U32 + 4 * U32 * np.where(some, np.abs(lse), 0.0))
     return out, lse, out_tol, lse_tol
 
