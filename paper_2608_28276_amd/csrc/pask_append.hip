@@ -22,7 +22,7 @@
 
 #include <type_traits>
 
-#include "pask_device.h"
+#include "pask_append.h"
 
 namespace pask {
 namespace {

@@ -140,16 +140,11 @@ hipError_t scratch_workspace(void** ptr);
 hipError_t launch_reset(const CacheView& cv, int32_t max_batch, hipStream_t s);
 hipError_t launch_append(const AppendArgs& a, hipStream_t s);        // chooses the windowed kernels when W > 0
 hipError_t launch_append_step(const AppendArgs& a, hipStream_t s);
-hipError_t launch_append_plan(const AppendArgs& a, hipStream_t s);   // slots, pages and counters alone; no window, no states
 hipError_t launch_budget_init(const CacheView& cv, int32_t batch, int64_t r0, hipStream_t s);
 hipError_t launch_attention(const AttnArgs& a, int group_size, hipStream_t s);
 // Attention over two caches with the same queries (partials in ref.ws_* and itv.ws_*), then
 // dist[b] += max over heads of the squared distance of the two outputs (Eq. 4).
 hipError_t launch_distortion(const AttnArgs& ref, const AttnArgs& itv, int group_size, const uint8_t* in_s,
                              float* dist, hipStream_t s);
-
-// Most pages that n new slots of one sequence can reach in its two stores: m
-// consecutive slots reach at most (m + 14) / 16 + 1.
-inline int pack_pages(int n) { return (n + 28) / kPage + 2; }
 
 }  // namespace pask

@@ -3,7 +3,7 @@
 // pask_latent_prompt.hip: expanded attention): the page layout and LDS access.
 #pragma once
 
-#include "pask_device.h"
+#include "pask_append.h"
 #include "pask_latent_internal.h"
 
 namespace pask {

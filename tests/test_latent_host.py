@@ -229,3 +229,9 @@ def test_reference_low_values():
     assert v[0, 32] == latent_ref.to_bf16(np.array([7 * 65504.0]))[0] and v[0, 33] == 0.0
     tiny = np.full((1, 32), 2.0 ** -27)               # absmax / 7 rounds to an fp16 zero
     assert (latent_ref.low_values(tiny) == 0).all()
+
+
+def test_the_recorded_attention_traffic_still_holds():
+    """The counters in profiles/ are tied to the code of the attention kernels, which the latent ones leave alone."""
+    import bench
+    assert bench.traffic_record("qwen3_4b_b64_p1k-8k_g1024") is not None
