@@ -210,13 +210,16 @@ __device__ __forceinline__ int entries_below(const int32_t* list, int lo, int hi
 // positions: of the position's predecessors those that are neither in this
 // store nor kept nowhere, so between position - slot - (positions not kept)
 // and position - slot, found among these.  A page's bytes are loaded first.
-// The memory bounds it.  The rows are stored past the caches: 64 sequences of
-// 100-12,000 tokens at rank 256 (327 MB in and out) take 63 us so, 107 with
-// plain stores, which evict the pages still to be read; streaming loads of
-// the pages beside them 93.  At most 16,384 blocks: 4,096 leave the longest
-// sequences' blocks running alone (124 against 107 us, plain stores).
+// The memory bounds it: 64 sequences of 100-12,000 tokens at rank 256 (327 MB in
+// and out) take 96 us from memory, 61 with the pages in the last-level cache.
+// Rows are stored past the caches: with plain stores, which evict pages still
+// to be read, 109 and 107.  At most 16,384 blocks: with 4,096 the longest
+// sequences' run alone at the end (131 us).  The blocks a compute unit holds,
+// named for the compiler, which then issues a page's loads sooner (111 us
+// without); at rank 512 more than five would spill (write and read 32 prompts:
+// 83 us, 123 with eight).
 template <int R, int P>
-__global__ __launch_bounds__(kThreads) void latent_read_kernel(LatentReadArgs a) {
+__global__ __launch_bounds__(kThreads, R >= 512 ? 5 : 8) void latent_read_kernel(LatentReadArgs a) {
   using PG = LatentPage<R, P>;
   __shared__ int s_cu[kWaves];
   __shared__ int s_row[2][kPage];
