@@ -99,7 +99,7 @@ __device__ __forceinline__ void read_transposed8(uint32_t at, uint4 (&v)[8]) {
       "ds_read_b64_tr_b16 %9, %16 offset:%21\n\t"
       "ds_read_b64_tr_b16 %10, %16 offset:2560\n\t"
       "ds_read_b64_tr_b16 %11, %16 offset:%22\n\t"
-      "ds_read_b64_tr_b16 %12, %16 offset:3072\n\t"
+      "ds_read_b64_tr_b16 %12, %16 offset:%25\n\t"
       "ds_read_b64_tr_b16 %13, %16 offset:%23\n\t"
       "ds_read_b64_tr_b16 %14, %16 offset:3584\n\t"
       "ds_read_b64_tr_b16 %15, %16 offset:%24\n\t"
@@ -107,7 +107,7 @@ __device__ __forceinline__ void read_transposed8(uint32_t at, uint4 (&v)[8]) {
       : "=&v"(a[0]), "=&v"(b[0]), "=&v"(a[1]), "=&v"(b[1]), "=&v"(a[2]), "=&v"(b[2]), "=&v"(a[3]), "=&v"(b[3]),
         "=&v"(a[4]), "=&v"(b[4]), "=&v"(a[5]), "=&v"(b[5]), "=&v"(a[6]), "=&v"(b[6]), "=&v"(a[7]), "=&v"(b[7])
       : "v"(at), "n"(kStep), "n"(kStep + 512), "n"(kStep + 1024), "n"(kStep + 1536), "n"(kStep + 2048),
-        "n"(kStep + 2560), "n"(kStep + 3072), "n"(kStep + 3584)
+        "n"(kStep + 2560), "n"(kStep + 6 * 512), "n"(kStep + 3584), "n"(6 * 512)
       : "memory");
 #pragma unroll
   for (int k = 0; k < 8; ++k) v[k] = make_uint4(a[k].x, a[k].y, b[k].x, b[k].y);
