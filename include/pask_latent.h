@@ -16,7 +16,9 @@
  *             it; keys are (c_t, r_t) and values c_t for every head
  *             (pask_latent_decode_attn).
  *   expanded  (prompts): keys and values per head, from the expansion product
- *             of the latents (pask_latent_prompt_attn).
+ *             of the latents: of the persisted ones, read back with their
+ *             positions (pask_latent_prompt_attn_pos), or of every token
+ *             (pask_latent_prompt_attn).
  * The products with W_uk and W_uv are the caller's.
  *
  * Formats:
@@ -160,7 +162,10 @@ int pask_latent_decode_attn(const pask_policy* policy, pask_latent_cache* cache,
  * rows cu_k[b] .. cu_k[b + 1] - 1 (int32 [batch + 1] each, device).  With n_q
  * and n_k rows, query i sees the keys j <= i + (n_k - n_q): the queries are the
  * last n_q tokens of the sequence, so a prompt's later chunk follows its
- * earlier ones (with n_k < n_q the first queries see nothing).  For head h < n_heads
+ * earlier ones (with n_k < n_q the first queries see nothing).  That is so where
+ * every token of the chunk has a row among the keys; over the rows of a
+ * read-back, which lack the tokens the table dropped, use
+ * pask_latent_prompt_attn_pos.  For head h < n_heads
  *   q_dev   bf16 [total_q][n_heads][nope_dim + rope_dim]
  *   kv_dev  bf16 [total_k][n_heads][nope_dim + v_dim]   (key part, then value)
  *   r_dev   bf16 [total_k][rope_dim]                    (shared by the heads)
@@ -185,6 +190,23 @@ int pask_latent_prompt_attn(int32_t batch, int32_t n_heads, int32_t nope_dim, in
                             int32_t max_q, int32_t total_q, int32_t total_k, const int32_t* cu_q_dev,
                             const int32_t* cu_k_dev, const void* q_dev, const void* kv_dev, const void* r_dev,
                             void* out_dev, float* lse_dev, float softmax_scale, hipStream_t stream);
+
+/* pask_latent_prompt_attn over keys at given positions, as pask_latent_read
+ * returns them: pos_dev int32 [total_k], not descending within a sequence, and
+ * q_first_dev int32 [batch], the position of each sequence's first query.  Query
+ * i of sequence b sees the keys of the sequence at positions
+ * <= q_first[b] + i: the persisted entries that a decode step at that position
+ * would attend.  A token that the table dropped is seen by no query, its own
+ * neither.  (With positions that do descend it is not said which keys are seen;
+ * nothing outside the sequence is.)
+ *
+ * Errors: as pask_latent_prompt_attn; PASK_E_ARG also for q_first_dev null,
+ * pos_dev null with total_k > 0, or either not 4-byte aligned. */
+int pask_latent_prompt_attn_pos(int32_t batch, int32_t n_heads, int32_t nope_dim, int32_t rope_dim, int32_t v_dim,
+                                int32_t max_q, int32_t total_q, int32_t total_k, const int32_t* cu_q_dev,
+                                const int32_t* cu_k_dev, const int32_t* pos_dev, const int32_t* q_first_dev,
+                                const void* q_dev, const void* kv_dev, const void* r_dev, void* out_dev,
+                                float* lse_dev, float softmax_scale, hipStream_t stream);
 
 /* Counters of the cache, as pask_cache_stats (without per_seq_group_head). */
 int pask_latent_cache_stats(const pask_policy* policy, const pask_latent_cache* cache, int32_t batch,

@@ -191,20 +191,6 @@ __global__ __launch_bounds__(128) void latent_step_kernel(AppendArgs a) {
   }
 }
 
-// Entries of an ascending list below x, known to be lo or more and hi or fewer:
-// 16 lanes of a wave together, 16 entries at a time.
-__device__ __forceinline__ int entries_below(const int32_t* list, int lo, int hi, int x) {
-  const int lane = (int)threadIdx.x & 63, l = lane & 15;
-  while (lo < hi) {
-    const int step = (hi - lo + 15) >> 4, at = lo + (l + 1) * step - 1;
-    const bool below = at < hi && list[at] < x;
-    const int c = __popc((uint32_t)(__ballot(below) >> (lane & 48)) & 0xFFFFu);
-    lo = min(lo + c * step, hi);
-    hi = min(lo + step - 1, hi);
-  }
-  return lo;
-}
-
 // Block (x, b) takes pages x, x + gridDim.x, ... of sequence b, HIGH's first.
 // A slot's row is cu[b] + its slot + the entries of the other store at lower
 // positions: of the position's predecessors those that are neither in this

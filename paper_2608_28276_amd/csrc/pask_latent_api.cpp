@@ -126,6 +126,48 @@ bool rows_ok(const void* p) { return p && aligned(p, 16); }
 float scale_log2(float softmax_scale) { return (float)((double)softmax_scale * 1.4426950408889634); }
 bool scale_ok(float softmax_scale) { return isfinite(softmax_scale) && isfinite(scale_log2(softmax_scale)); }
 
+int check_prompt(int32_t batch, int32_t n_heads, int32_t nope_dim, int32_t rope_dim, int32_t v_dim, int32_t max_q,
+                 int32_t total_q, int32_t total_k, const int32_t* cu_q, const int32_t* cu_k, const float* lse,
+                 float softmax_scale) {
+  if (batch < 1 || batch > 65535 || n_heads < 1 || n_heads > PASK_LATENT_MAX_HEADS) return PASK_E_SHAPE;
+  if ((nope_dim != 64 && nope_dim != 128) || (v_dim != 64 && v_dim != 128) || (rope_dim != 32 && rope_dim != 64))
+    return PASK_E_SHAPE;
+  if (max_q < 0 || total_q < 0 || total_k < 0 || !scale_ok(softmax_scale)) return PASK_E_ARG;
+  if (!cu_q || !cu_k || !aligned(cu_q, 4) || !aligned(cu_k, 4) || !aligned(lse, 4)) return PASK_E_ARG;
+  return PASK_OK;
+}
+
+// Prompts with queries, their sizes and offsets checked (check_prompt); pos: null, or the keys' positions.
+int prompt_attn(const char* where, int32_t batch, int32_t n_heads, int32_t nope_dim, int32_t rope_dim, int32_t v_dim,
+                int32_t max_q, int32_t total_q, int32_t total_k, const int32_t* cu_q, const int32_t* cu_k,
+                const int32_t* pos, const int32_t* q_first, const void* q, const void* kv, const void* r, void* out,
+                float* lse, float softmax_scale, hipStream_t stream) {
+  if (!rows_ok(q) || !rows_ok(out)) return PASK_E_ARG;
+  if (total_k > 0 && (!rows_ok(kv) || !rows_ok(r))) return PASK_E_ARG;
+  pask::LatentPromptArgs a;
+  a.q = static_cast<const uint16_t*>(q);
+  a.kv = static_cast<const uint16_t*>(kv);
+  a.r = static_cast<const uint16_t*>(r);
+  a.out = static_cast<uint16_t*>(out);
+  a.lse = lse;
+  a.cu_q = cu_q;
+  a.cu_k = cu_k;
+  a.pos = pos;
+  a.q_first = q_first;
+  a.scale_log2 = scale_log2(softmax_scale);
+  a.batch = batch;
+  a.heads = n_heads;
+  a.nope = nope_dim;
+  a.rope = rope_dim;
+  a.v = v_dim;
+  a.max_q = std::min(max_q, total_q);
+  a.total_q = total_q;
+  a.total_k = total_k;
+  if (pask::latent_prompt_blocks(a) > (1 << 23) - 1) return PASK_E_SHAPE;   // a launch holds 2^32 - 1 threads
+  const hipError_t e = pask::launch_latent_prompt(a, stream);
+  return pask::debug_check_words(where, e == hipSuccess ? PASK_OK : PASK_E_HIP, nullptr, 0, stream);
+}
+
 }  // namespace
 
 extern "C" {
@@ -251,35 +293,28 @@ int pask_latent_prompt_attn(int32_t batch, int32_t n_heads, int32_t nope_dim, in
                             int32_t max_q, int32_t total_q, int32_t total_k, const int32_t* cu_q_dev,
                             const int32_t* cu_k_dev, const void* q_dev, const void* kv_dev, const void* r_dev,
                             void* out_dev, float* lse_dev, float softmax_scale, hipStream_t stream) {
-  if (batch < 1 || batch > 65535 || n_heads < 1 || n_heads > PASK_LATENT_MAX_HEADS) return PASK_E_SHAPE;
-  if ((nope_dim != 64 && nope_dim != 128) || (v_dim != 64 && v_dim != 128) || (rope_dim != 32 && rope_dim != 64))
-    return PASK_E_SHAPE;
-  if (max_q < 0 || total_q < 0 || total_k < 0 || !scale_ok(softmax_scale)) return PASK_E_ARG;
-  if (!cu_q_dev || !cu_k_dev || !aligned(cu_q_dev, 4) || !aligned(cu_k_dev, 4) || !aligned(lse_dev, 4))
-    return PASK_E_ARG;
+  const int st = check_prompt(batch, n_heads, nope_dim, rope_dim, v_dim, max_q, total_q, total_k, cu_q_dev, cu_k_dev,
+                              lse_dev, softmax_scale);
+  if (st != PASK_OK || max_q == 0 || total_q == 0) return st;
+  return prompt_attn("pask_latent_prompt_attn", batch, n_heads, nope_dim, rope_dim, v_dim, max_q, total_q, total_k,
+                     cu_q_dev, cu_k_dev, nullptr, nullptr, q_dev, kv_dev, r_dev, out_dev, lse_dev, softmax_scale,
+                     stream);
+}
+
+int pask_latent_prompt_attn_pos(int32_t batch, int32_t n_heads, int32_t nope_dim, int32_t rope_dim, int32_t v_dim,
+                                int32_t max_q, int32_t total_q, int32_t total_k, const int32_t* cu_q_dev,
+                                const int32_t* cu_k_dev, const int32_t* pos_dev, const int32_t* q_first_dev,
+                                const void* q_dev, const void* kv_dev, const void* r_dev, void* out_dev,
+                                float* lse_dev, float softmax_scale, hipStream_t stream) {
+  const int st = check_prompt(batch, n_heads, nope_dim, rope_dim, v_dim, max_q, total_q, total_k, cu_q_dev, cu_k_dev,
+                              lse_dev, softmax_scale);
+  if (st != PASK_OK) return st;
+  if (!q_first_dev || !aligned(q_first_dev, 4) || !aligned(pos_dev, 4)) return PASK_E_ARG;
+  if (total_k > 0 && !pos_dev) return PASK_E_ARG;
   if (max_q == 0 || total_q == 0) return PASK_OK;
-  if (!rows_ok(q_dev) || !rows_ok(out_dev)) return PASK_E_ARG;
-  if (total_k > 0 && (!rows_ok(kv_dev) || !rows_ok(r_dev))) return PASK_E_ARG;
-  pask::LatentPromptArgs a;
-  a.q = static_cast<const uint16_t*>(q_dev);
-  a.kv = static_cast<const uint16_t*>(kv_dev);
-  a.r = static_cast<const uint16_t*>(r_dev);
-  a.out = static_cast<uint16_t*>(out_dev);
-  a.lse = lse_dev;
-  a.cu_q = cu_q_dev;
-  a.cu_k = cu_k_dev;
-  a.scale_log2 = scale_log2(softmax_scale);
-  a.batch = batch;
-  a.heads = n_heads;
-  a.nope = nope_dim;
-  a.rope = rope_dim;
-  a.v = v_dim;
-  a.max_q = std::min(max_q, total_q);
-  a.total_q = total_q;
-  a.total_k = total_k;
-  if (pask::latent_prompt_blocks(a) > (1 << 23) - 1) return PASK_E_SHAPE;   // a launch holds 2^32 - 1 threads
-  const hipError_t e = pask::launch_latent_prompt(a, stream);
-  return pask::debug_check_words("pask_latent_prompt_attn", e == hipSuccess ? PASK_OK : PASK_E_HIP, nullptr, 0, stream);
+  return prompt_attn("pask_latent_prompt_attn_pos", batch, n_heads, nope_dim, rope_dim, v_dim, max_q, total_q, total_k,
+                     cu_q_dev, cu_k_dev, pos_dev, q_first_dev, q_dev, kv_dev, r_dev, out_dev, lse_dev, softmax_scale,
+                     stream);
 }
 
 int pask_latent_cache_stats(const pask_policy* policy, const pask_latent_cache* cache, int32_t batch,

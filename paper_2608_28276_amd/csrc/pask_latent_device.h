@@ -1,6 +1,7 @@
 // Shared by the latent-attention kernels (pask_latent.hip: persisting and
 // reading back; pask_latent_attn.hip: absorbed decode attention;
-// pask_latent_prompt.hip: expanded attention): the page layout and LDS access.
+// pask_latent_prompt.hip: expanded attention): the page layout, the search of a
+// list of positions and LDS access.
 #pragma once
 
 #include "pask_append.h"
@@ -47,6 +48,20 @@ __device__ __forceinline__ uint4 low_values(uint32_t w, float s) {
                     pack_bf16x2(v(hi, 0), v(hi, 1)), pack_bf16x2(v(hi, 2), v(hi, 3)));
 }
 __device__ __forceinline__ float half_value(uint16_t h) { return (float)__builtin_bit_cast(_Float16, h); }
+
+// Entries of an ascending list below x, known to be lo or more and hi or fewer:
+// 16 lanes of a wave together, 16 entries at a time.
+__device__ __forceinline__ int entries_below(const int32_t* list, int lo, int hi, int x) {
+  const int lane = (int)threadIdx.x & 63, l = lane & 15;
+  while (lo < hi) {
+    const int step = (hi - lo + 15) >> 4, at = lo + (l + 1) * step - 1;
+    const bool below = at < hi && list[at] < x;
+    const int c = __popc((uint32_t)(__ballot(below) >> (lane & 48)) & 0xFFFFu);
+    lo = min(lo + c * step, hi);
+    hi = min(lo + step - 1, hi);
+  }
+  return lo;
+}
 
 // x, which the compiler takes for new (no code): what follows from it is made
 // where it is used, not kept in registers through the loops around.

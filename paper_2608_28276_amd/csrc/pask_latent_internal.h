@@ -41,6 +41,8 @@ struct LatentPromptArgs {
   float* lse;               // [total_q][heads] or null
   const int32_t* cu_q;
   const int32_t* cu_k;
+  const int32_t* pos;       // [total_k] positions of the keys, or null: the queries are the last of their keys
+  const int32_t* q_first;   // [batch] position of each sequence's first query, with pos
   float scale_log2;
   int32_t batch, heads, nope, rope, v, max_q, total_q, total_k;
 };

@@ -87,6 +87,10 @@ __device__ __forceinline__ void add_seen_values(const uint8_t* s_v, f32x16_t s, 
 // ones, so that the matrix and the vector units work at once; two steps of keys
 // and values are on their way into a ring of three LDS buffers meanwhile.
 // Rows past the sequence repeat its last one: no query sees them.
+// The keys a query sees are the first ones of its sequence, as many as its place
+// from the end allows or, where the keys come with positions, as lie at its
+// position or before (8,192 queries and keys of 32 heads: 699 us by place, 710
+// by position).
 // Bound by the matrix cores and the exponentials beside them: 8,192 queries and
 // keys, 32 heads of 128 + 64 and values of 128 take 697-743 us from card to card
 // (687 GFLOP, 925-986 TFLOP/s); this loop's products alone take 516.
@@ -108,7 +112,9 @@ __global__ __launch_bounds__(64 * W, 2) void latent_prompt_kernel(LatentPromptAr
   // The longest tiles first: the last of every sequence before the ones before
   // it, or by the keys they see where there are few enough to rank in a wave's
   // lanes (with more the rest evens out; 8 chunks of 266-1,024 queries with up
-  // to 2,306 keys before them, 20 heads: 208 us by the first, 168 so).
+  // to 2,306 keys before them, 20 heads: 208 us by the first, 168 so).  With
+  // positions too these are the keys by the place from the end, the fewest they
+  // can be: the order only has to be good.
   const int items = q_tiles * a.batch;
   if (items <= 64) {
     const int b = lane % a.batch, tile = q_tiles - 1 - lane / a.batch;
@@ -130,9 +136,21 @@ __global__ __launch_bounds__(64 * W, 2) void latent_prompt_kernel(LatentPromptAr
   if (tile * kRows >= nq_in) return;
   const int row0 = tile * kRows + wave * 32, row = row0 + n;   // this lane's query
   const int past = nk - nq;
-  const int last = min(tile * kRows + kRows, nq_in) - 1;       // the tile's last query
-  const int n_see = min(nk, last + past + 1);                  // keys it sees; may be <= 0
-  const int steps = n_see > 0 ? (n_see + kKeys - 1) / kKeys : 0;
+  // Keys that the tile's last query, the wave's first and its last see: by their place from the end, or those at their
+  // position and before, found by 16 lanes each.
+  const int tile_last = min(tile * kRows + kRows, nq_in) - 1, wave_last = min(row0 + 31, nq_in - 1);
+  auto by_place = [&](int i) { return min(max(i + past + 1, 0), nk); };
+  auto position = [&](int i) { return (long long)a.q_first[b] + i; };
+  int n_see = by_place(tile_last), first_sees = by_place(row0), last_sees = by_place(wave_last);
+  if (a.pos) {
+    const long long at = position(lane < 16 ? tile_last : lane < 32 ? row0 : wave_last);
+    const int seen = at >= INT32_MAX ? nk : entries_below(a.pos + k0, 0, nk, (int)at + 1);
+    n_see = __builtin_amdgcn_readlane(seen, 0);
+    first_sees = __builtin_amdgcn_readlane(seen, 16);
+    last_sees = __builtin_amdgcn_readlane(seen, 32);
+  }
+  if (row0 >= nq_in) first_sees = last_sees = 0;
+  const int steps = (n_see + kKeys - 1) / kKeys;
 
   // Scores are scaled by |scale|; its sign goes to the queries, so that a score's maximum is a scaled one's.
   uint4 qf[KI];
@@ -265,7 +283,7 @@ __global__ __launch_bounds__(64 * W, 2) void latent_prompt_kernel(LatentPromptAr
   // The units that all queries of the wave see whole: unit i's scores s become
   // weights beside the scores of unit i + 1.  The loop is left to move the
   // reference: in it the sums are only added to.
-  const int whole = row0 < nq_in ? min(units, max(0, (row0 + past + 1) / 32)) : 0;
+  const int whole = min(units, first_sees / 32);
   float base = 0.0f, odd_sum = 0.0f, top = -INFINITY;
   auto turn = [&](int i, f32x16_t& s, f32x16_t& next) {
     const uint32_t nkvs = step_of(i + 1), nu = (i + 1) & 1;
@@ -352,10 +370,19 @@ __global__ __launch_bounds__(64 * W, 2) void latent_prompt_kernel(LatentPromptAr
     }
   }
   // Units at the edge: some query of the wave does not see all their keys.
+  int sees = row + past + 1;                       // keys that this query sees
+  if (a.pos) {                                     // between the wave's first and last query's
+    sees = first_sees;
+    for (int end = last_sees; sees < end;) {
+      const int mid = (sees + end) >> 1;
+      if (a.pos[k0 + mid] <= position(row)) sees = mid + 1;
+      else end = mid;
+    }
+  }
   for (; i < units; ++i) {
-    if (row0 < nq_in && row0 + 31 + past >= 32 * i) {          // some query of the wave sees a key
+    if (last_sees > 32 * i) {                      // some query of the wave sees a key
       const uint8_t* s_v = s_kv[(i >> 1) % 3] + kKn + kKr + (i & 1) * 32 * VC * 16;
-      const int see = row + past - 32 * i;         // this query sees the unit's keys 0 .. see
+      const int see = sees - 1 - 32 * i;           // this query sees the unit's keys 0 .. see
       auto hidden = [&](int r) { return 8 * (r >> 2) + 4 * g + (r & 3) > see; };
       s = scores(step_of(i), i & 1);
 #pragma unroll

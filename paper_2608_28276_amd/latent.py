@@ -1,7 +1,8 @@
 """Python binding of the latent-attention entry points of libpask.so, declared
 in include/pask_latent.h: one function per entry point with the same name, on
 the statuses, policies and pointer rules of the `pask` module.  prompt_attn()
-is pask_latent_prompt_attn for torch tensors, shapes taken from them.
+is pask_latent_prompt_attn, or pask_latent_prompt_attn_pos, for torch tensors,
+shapes taken from them.
 """
 
 from __future__ import annotations
@@ -16,7 +17,8 @@ from .pask import _check, _ptr
 
 EXPORTS = ("pask_latent_cache_layout_query", "pask_latent_cache_bytes", "pask_latent_cache_init",
            "pask_latent_cache_reset", "pask_latent_append", "pask_latent_read", "pask_latent_workspace_bytes",
-           "pask_latent_decode_attn", "pask_latent_prompt_attn", "pask_latent_cache_stats")
+           "pask_latent_decode_attn", "pask_latent_prompt_attn", "pask_latent_prompt_attn_pos",
+           "pask_latent_cache_stats")
 PASK_LATENT_MAX_HEADS = 128
 
 
@@ -44,6 +46,7 @@ _lib.pask_latent_workspace_bytes.argtypes = [_G, _I, _I]
 _lib.pask_latent_decode_attn.argtypes = [_POL, _CACHE, _I, _I, _P, _P, _P, _P, _P, _P, C.c_float, _I, _P, C.c_size_t,
                                          _P]
 _lib.pask_latent_prompt_attn.argtypes = [_I] * 8 + [_P] * 7 + [C.c_float, _P]
+_lib.pask_latent_prompt_attn_pos.argtypes = [_I] * 8 + [_P] * 9 + [C.c_float, _P]
 _lib.pask_latent_cache_stats.argtypes = [_POL, _CACHE, _I, C.POINTER(pask.pask_stats), _P]
 
 
@@ -107,6 +110,16 @@ def pask_latent_prompt_attn(batch: int, n_heads: int, nope_dim: int, rope_dim: i
            "pask_latent_prompt_attn")
 
 
+def pask_latent_prompt_attn_pos(batch: int, n_heads: int, nope_dim: int, rope_dim: int, v_dim: int, max_q: int,
+                                total_q: int, total_k: int, cu_q, cu_k, pos, q_first, q, kv, r, out, lse=None,
+                                softmax_scale: float = 1.0, stream=0) -> None:
+    _check(_lib.pask_latent_prompt_attn_pos(int(batch), int(n_heads), int(nope_dim), int(rope_dim), int(v_dim),
+                                            int(max_q), int(total_q), int(total_k), _ptr(cu_q), _ptr(cu_k), _ptr(pos),
+                                            _ptr(q_first), _ptr(q), _ptr(kv), _ptr(r), _ptr(out), _ptr(lse),
+                                            float(softmax_scale), _ptr(stream)),
+           "pask_latent_prompt_attn_pos")
+
+
 def pask_latent_cache_stats(policy, cache: pask_latent_cache, batch: int, stream=0):
     """Returns (stats, status); status is PASK_OK or PASK_E_DEVICE_FLAG."""
     out = pask.pask_stats()
@@ -127,12 +140,15 @@ def check_tensor(name: str, t, dtype, shape, device) -> None:
         raise pask.PaskError(pask.PASK_E_SHAPE, f"{name}: shape {tuple(shape)} expected, got {tuple(t.shape)}")
 
 
-def prompt_attn(q, kv, r, out, lse, cu_q, cu_k, max_q: int, softmax_scale: float | None = None) -> None:
+def prompt_attn(q, kv, r, out, lse, cu_q, cu_k, max_q: int, softmax_scale: float | None = None, pos=None,
+                q_first=None) -> None:
     """Causal attention of packed prompts in the expanded form, on q's device and its current stream.
 
     q bf16 [total_q, heads, nope + rope], kv bf16 [total_k, heads, nope + v], r bf16 [total_k, rope], out bf16
-    [total_q, heads, v], lse fp32 [total_q, heads] or None, cu_q and cu_k int32 [batch + 1]; sequence b's queries are
-    the last of its keys.  softmax_scale: 1 / sqrt(nope + rope) when None."""
+    [total_q, heads, v], lse fp32 [total_q, heads] or None, cu_q and cu_k int32 [batch + 1].  Sequence b's queries are
+    the last of its keys; or, with pos int32 [total_k] (the keys' positions, as the cache's read-back returns them) and
+    q_first int32 [batch] (the position of each sequence's first query), query i sees the keys at q_first[b] + i and
+    before.  softmax_scale: 1 / sqrt(nope + rope) when None."""
     for name, t in (("q", q), ("kv", kv), ("r", r), ("out", out), ("cu_q", cu_q), ("cu_k", cu_k)):
         if not isinstance(t, torch.Tensor):
             raise pask.PaskError(pask.PASK_E_ARG, f"{name}: a tensor expected, got {type(t).__name__}")
@@ -153,7 +169,15 @@ def prompt_attn(q, kv, r, out, lse, cu_q, cu_k, max_q: int, softmax_scale: float
     check_tensor("cu_k", cu_k, torch.int32, (batch + 1,), dev)
     if lse is not None:
         check_tensor("lse", lse, torch.float32, (total_q, heads), dev)
+    sizes = (batch, heads, nope, rope, v, max_q, total_q, kv.shape[0])
+    scale = 1.0 / math.sqrt(qk) if softmax_scale is None else softmax_scale
+    if pos is None and q_first is None:
+        with torch.cuda.device(dev):
+            pask_latent_prompt_attn(*sizes, cu_q, cu_k, q, kv, r, out, lse, scale,
+                                    torch.cuda.current_stream(dev).cuda_stream)
+        return
+    check_tensor("pos", pos, torch.int32, (kv.shape[0],), dev)
+    check_tensor("q_first", q_first, torch.int32, (batch,), dev)
     with torch.cuda.device(dev):
-        pask_latent_prompt_attn(batch, heads, nope, rope, v, max_q, total_q, kv.shape[0], cu_q, cu_k, q, kv, r, out, lse,
-                                1.0 / math.sqrt(qk) if softmax_scale is None else softmax_scale,
-                                torch.cuda.current_stream(dev).cuda_stream)
+        pask_latent_prompt_attn_pos(*sizes, cu_q, cu_k, pos, q_first, q, kv, r, out, lse, scale,
+                                    torch.cuda.current_stream(dev).cuda_stream)

@@ -319,9 +319,17 @@ class PaskLatentSession:
         self._call(latent.pask_latent_decode_attn, self.policy, self.cache, layer, b, q, out, lse, tags_new, c_new,
                    r_new, self.softmax_scale, max_ctx_hint or self.max_ctx_hint, self.ws, self.ws_bytes)
 
-    def prompt(self, q, kv, r, out, lse, cu_q, cu_k, max_q: int):
-        """latent.prompt_attn with the session's softmax scale."""
-        latent.prompt_attn(q, kv, r, out, lse, cu_q, cu_k, max_q, self.softmax_scale)
+    def prompt(self, q, kv, r, out, lse, cu_q, cu_k, max_q: int, pos=None, q_first=None):
+        """latent.prompt_attn with the session's softmax scale.  Over rows that read() returned, pos is their pos_out
+        and q_first what next_positions() gave before the queries' tokens were appended."""
+        latent.prompt_attn(q, kv, r, out, lse, cu_q, cu_k, max_q, self.softmax_scale, pos, q_first)
+
+    def next_positions(self, layer: int, batch: int | None = None):
+        """int32 [batch], a copy: the position that the next token of each sequence takes."""
+        b = self.geom.max_batch if batch is None else batch
+        if not (0 <= layer < self.geom.n_layers and 1 <= b <= self.geom.max_batch):
+            raise pask.PaskError(pask.PASK_E_SHAPE, "next_positions: layer or batch out of range")
+        return self.counters()[:b, layer, 2].clone(memory_format=torch.contiguous_format)
 
     def reset(self):
         self._call(latent.pask_latent_cache_reset, self.cache)
