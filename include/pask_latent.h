@@ -103,7 +103,8 @@ int pask_latent_cache_reset(pask_latent_cache* cache, hipStream_t stream);
  * PASK_APPEND_KEEP_ALL.
  *
  * Errors: PASK_E_ARG (null or misaligned pointers: c_dev, r_dev 16 bytes,
- * n_new_dev 4; flags), PASK_E_SHAPE (layer, batch or max_new out of range,
+ * n_new_dev 4; flags), PASK_E_SHAPE (layer, batch or max_new out of range, or
+ * max_new above 2^28 - 61, whose pages are more than one launch fills;
  * policy / geometry mismatch), PASK_E_POLICY, PASK_E_UNSUPPORTED (policy with a
  * recent window), PASK_E_HIP. */
 int pask_latent_append(const pask_policy* policy, pask_latent_cache* cache, int32_t layer, int32_t batch,

@@ -210,6 +210,7 @@ int pask_latent_append(const pask_policy* policy, pask_latent_cache* cache, int3
   if (st == PASK_OK) st = check_call(cache, layer, batch);
   if (st != PASK_OK) return st;
   if (max_new < 0 || max_new > cache->geom.max_tokens_per_seq) return PASK_E_SHAPE;
+  if (!pask::append_fits(max_new, 0)) return PASK_E_SHAPE;
   if (flags & ~(uint32_t)PASK_APPEND_KEEP_ALL) return PASK_E_ARG;
   if (!rows_ok(c_dev) || !rows_ok(r_dev)) return PASK_E_ARG;
   if (!tags_dev && !(flags & PASK_APPEND_KEEP_ALL)) return PASK_E_ARG;
