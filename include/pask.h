@@ -279,9 +279,10 @@ int pask_cache_reset(pask_cache* cache, hipStream_t stream);
  * nor charged.
  *
  * Errors: PASK_E_ARG (null or misaligned pointers, flags), PASK_E_SHAPE
- * (layer, batch or max_new out of range, policy / geometry mismatch),
- * PASK_E_POLICY (states given to a policy without the controller),
- * PASK_E_HIP. */
+ * (layer, batch or max_new out of range, or a bulk call with max_new +
+ * recent_window above 2^28 - 61 or both above 2^24 - 1, more than one launch
+ * fills; policy / geometry mismatch), PASK_E_POLICY (states given to a policy
+ * without the controller), PASK_E_HIP. */
 int pask_kv_append(const pask_policy* policy, pask_cache* cache, int32_t layer, int32_t batch,
                    const int32_t* n_new_dev, int32_t max_new, const uint8_t* tags_dev,
                    const uint8_t* states_dev, const void* k_dev, const void* v_dev, uint32_t flags,

@@ -370,6 +370,8 @@ int pask_kv_append(const pask_policy* policy, pask_cache* cache, int32_t layer, 
   if (layer < 0 || layer >= g.n_layers) return PASK_E_SHAPE;
   if (batch < 1 || batch > g.max_batch) return PASK_E_SHAPE;
   if (max_new < 0 || max_new > g.max_tokens_per_seq) return PASK_E_SHAPE;
+  const bool one_token = max_new == 1 && !n_new_dev;   // has a kernel of its own, one workgroup per sequence
+  if (max_new > 0 && !one_token && !pask::append_fits(max_new, g.recent_window)) return PASK_E_SHAPE;
   if (flags & ~(uint32_t)PASK_APPEND_KEEP_ALL) return PASK_E_ARG;
   if (!k_dev || !v_dev || !aligned(k_dev, 16) || !aligned(v_dev, 16)) return PASK_E_ARG;
   if (!tags_dev && !(flags & PASK_APPEND_KEEP_ALL)) return PASK_E_ARG;
