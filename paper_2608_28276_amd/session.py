@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import math
 import struct
+import weakref
 
 import torch
 
@@ -216,6 +217,13 @@ class PaskSession:
         return fix(kc), fix(ks).astype(np.int64), fix(vc), fix(vs).astype(np.int64)
 
 
+class LatentState:
+    """What PaskLatentSession.save() returns, for its restore(): valid while it has the session's key."""
+
+    def __init__(self, head: torch.Tensor, serial: int, key: object, captured: bool):
+        self._head, self._serial, self._key, self._captured = head, serial, key, captured
+
+
 class PaskLatentSession:
     """One latent cache of `max_batch` sequences x `n_layers` layers on one GPU,
     its workspace and its calls (include/pask_latent.h).  Calls run on the
@@ -250,6 +258,8 @@ class PaskLatentSession:
         if prefill is not None:
             self.buf.fill_(prefill)
             self.ws.fill_(prefill)
+        self._saved, self._key = weakref.WeakSet(), object()   # the states that restore() takes, and their key,
+        self._serial = self._newest = 0              # the number of the last one saved, of the newest valid one
         self.cache = latent.pask_latent_cache()
         self._call(latent.pask_latent_cache_init, self.cache, self.geom, self.buf, self.nbytes)
 
@@ -332,6 +342,8 @@ class PaskLatentSession:
         return self.counters()[:b, layer, 2].clone(memory_format=torch.contiguous_format)
 
     def reset(self):
+        """Empty every sequence; voids what save() returned before."""
+        self._saved, self._key = weakref.WeakSet(), object()
         self._call(latent.pask_latent_cache_reset, self.cache)
 
     def stats(self, batch: int | None = None):
@@ -339,17 +351,34 @@ class PaskLatentSession:
         return self._call(latent.pask_latent_cache_stats, self.policy, self.cache, batch or self.geom.max_batch)
 
     # -- going back, as after a rejected draft --------------------------------
+    def _capturing(self) -> bool:
+        return self._call(lambda stream: torch.cuda.is_current_stream_capturing())
+
     def _head(self):
         return self.buf[:self.layout.block_table_off]
 
-    def save(self):
+    def save(self) -> LatentState:
         """The state of every sequence and layer as it is now, for restore(): the counts, cursors and flags (pages are
-        only added to, and what lies past the counts is written again before it is read)."""
-        return self._head().clone()
+        only added to, and what lies past the counts is written again before it is read).  Saved while a graph is
+        captured, it is for restore() in the same capture alone: no bytes are there before a replay."""
+        self._newest = self._serial = self._serial + 1
+        state = LatentState(self._head().clone(), self._serial, self._key, self._capturing())
+        self._saved.add(state)
+        return state
 
-    def restore(self, saved):
-        """Back to the state save() returned, on the same stream; void after a reset() in between."""
-        self._head().copy_(saved)
+    def restore(self, saved: LatentState):
+        """Back to a state that save() returned, on the same stream, as often as wanted.  Going back voids the states
+        saved after it (their pages are handed out again), and a reset() all of them: a void state, or another
+        session's, raises PaskError.  The check is made when restore() is called, not when a graph that captured it is
+        replayed: replay it only while the state is valid."""
+        if getattr(saved, "_key", None) is not self._key or (saved._captured and not self._capturing()):
+            raise pask.PaskError(pask.PASK_E_ARG, "restore: not a state of this session, or void")
+        if self._newest > saved._serial:
+            for later in [s for s in self._saved if s._serial > saved._serial]:
+                later._key = None
+                self._saved.discard(later)
+            self._newest = saved._serial
+        self._head().copy_(saved._head)
 
     # -- views of the cache buffer (inspection) -----------------------------
     def counters(self):
