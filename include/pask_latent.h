@@ -31,6 +31,15 @@
  *                same cache.
  *   Inputs are taken as finite; a non-finite latent kept HIGH is kept as it is.
  *
+ * Numerics of both attentions: scores, softmax statistics and all sums in fp32;
+ * a softmax weight is rounded once to bf16 (half a step, 2^-8 of it) for its
+ * product with the value, its sum is kept of the unrounded ones.  Weights are
+ * taken relative to a reference that a score may exceed by 16 in base 2 before
+ * it moves, so sums of values reach 2^16 times their result: an output element
+ * is certain to be finite where the query's scores, and the sums they are made
+ * of, are finite in fp32 and the magnitudes of its values, over the entries that
+ * the query sees, sum to less than 2^112 (5e33).
+ *
  * Not here: the recent window (a policy whose recent_window is not 0 is
  * refused with PASK_E_UNSUPPORTED) and the online controller (Eq. 10 decides
  * every token; a policy's controller section is ignored).

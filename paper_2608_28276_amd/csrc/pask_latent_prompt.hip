@@ -19,9 +19,12 @@ typedef float f32x16_t __attribute__((ext_vector_type(16)));
 constexpr int kKeys = 64;                          // keys of a step
 // The reference of a query's weights moves only when a score exceeds it by more
 // than this (in base 2).  Weights up to 2^16 and their sums are as precise as
-// weights below 1 (bf16 and fp32 have the same exponents), and stay far from the
-// largest fp32; a reference that follows every maximum costs a multiplication of
-// all sums in the loop, which the compiler answers with copies of them.
+// weights below 1 (bf16 and fp32 have the same exponents); the sums stay below the
+// largest fp32 for values that sum to less than 2^112, the bound the header
+// gives.  (A reference 2^16 higher would trade that for entries lost at 2^-110 of
+// the largest weight in place of 2^-126.)  A reference that follows every maximum
+// costs a multiplication of all sums in the loop, which the compiler answers with
+// copies of them.
 constexpr float kHeadroom = 16.0f;
 constexpr int kAhead = 4;                          // score operands read ahead of their product
 constexpr float kLn2 = 0.6931471805599453f;
