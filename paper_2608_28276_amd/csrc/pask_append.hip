@@ -347,6 +347,9 @@ __global__ __launch_bounds__(kPlanThreads) void append_plan_kernel(AppendArgs a)
   // tags it does come with are still looked at for ones outside the table.
   const uint8_t* tags = a.tags ? a.tags + (size_t)b * a.max_new : nullptr;
   const unsigned pool[2] = {(unsigned)cv.hi_pages, (unsigned)cv.lo_pages};
+  // The cursors of pools that were full when the call began stay: counted on with
+  // every token that finds no page, they would come round to the first page.
+  const unsigned cursor0 = threadIdx.x < 2 ? cv.status[2 + threadIdx.x] : 0u;
   __syncthreads();
 
   // Between two chunks: the words a chunk shares (s_wave, s_page_base,
@@ -417,7 +420,7 @@ __global__ __launch_bounds__(kPlanThreads) void append_plan_kernel(AppendArgs a)
       unsigned base = 0u;
       int granted = 0;
       if (opens > 0) {
-        base = atomicAdd(&cv.status[2 + s], (unsigned)opens);
+        base = cursor0 >= limit ? cursor0 : atomicAdd(&cv.status[2 + s], (unsigned)opens);
         granted = base >= limit ? 0 : (int)min((unsigned)opens, limit - base);
       }
       s_page_base[s] = base;

@@ -130,6 +130,7 @@ __global__ __launch_bounds__(128) void latent_step_kernel(AppendArgs a) {
     uint32_t flags = 0;
     int32_t* cnt = counters_of(cv, b, a.layer);
     const int pos = cnt[kCntPos], slots[2] = {cnt[kCntHi], cnt[kCntLo]};
+    const unsigned cursors[2] = {cv.status[2], cv.status[3]};
     int code = -1, page = -1;
     if (pos >= cv.max_tokens) {
       flags |= PASK_FLAG_SEQ_CAPACITY;
@@ -148,8 +149,10 @@ __global__ __launch_bounds__(128) void latent_step_kernel(AppendArgs a) {
         int32_t* entry = block_table_of(cv, b, a.layer, st) + slot / kPage;
         bool stored = true;
         if (slot % kPage == 0) {
-          const unsigned pid = atomicAdd(&cv.status[2 + st], 1u);
-          stored = pid < (unsigned)(st == kHi ? cv.hi_pages : cv.lo_pages);
+          // A pool that was full when the call began keeps its cursor (append_plan_kernel).
+          const unsigned pages = (unsigned)(st == kHi ? cv.hi_pages : cv.lo_pages);
+          const unsigned pid = cursors[st] >= pages ? cursors[st] : atomicAdd(&cv.status[2 + st], 1u);
+          stored = pid < pages;
           page = (int)pid;
           if (stored) *entry = page;
         } else {

@@ -100,3 +100,24 @@ def test_a_tag_outside_the_table(kind):
     assert status == pask.PASK_E_DEVICE_FLAG and st.device_flags == pask.PASK_FLAG_BAD_TAG and st.n_lost == 0
     p.check_counters()
     p.check_read()
+
+
+@pytest.mark.parametrize("kind", ["bulk", "one", "step"])
+@pytest.mark.parametrize("action", [HIGH, LOW])
+def test_a_pool_full_for_long(action, kind):
+    """However many tokens a full pool has lost, its first page is not handed out again."""
+    p = Pair(batch=2, heads=5, rank=128, rope=32, max_tokens=64, hi_pages=2, lo_pages=2, action=[action], floor=[DROP],
+             seed=action + 20)
+    z = lambda n: (torch.zeros(2, n, dtype=torch.uint8),) + p.tokens(n)[1:]
+    p.append([16, 16], tokens=z(16))
+    at = p.sess.layout.status_off + 8 + 4 * (action == LOW)
+    cursor = p.sess.buf[at:at + 4].view(torch.int32)
+    cursor.fill_(-2)                                 # as after 2^32 - 4 tokens that found no page
+    for _ in range(3):
+        seen = add(p, kind, z(1))
+    st, status = p.sess.stats()
+    assert status == pask.PASK_E_DEVICE_FLAG and st.n_lost == 6 and st.n_high + st.n_low == 32
+    assert (st.hi_pages_used, st.lo_pages_used) == ((2, 0) if action == HIGH else (0, 2))
+    p.check_read()
+    if seen:
+        p.check_attention(*seen)
