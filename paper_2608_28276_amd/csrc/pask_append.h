@@ -3,14 +3,11 @@
 #pragma once
 
 #include "pask_device.h"
+#include "pask_pages.h"
 
 namespace pask {
 
 hipError_t launch_append_plan(const AppendArgs& a, hipStream_t s);   // slots, pages and counters alone; no window, no states
-
-// Most pages that n new slots of one sequence can reach in its two stores: m
-// consecutive slots reach at most (m + 14) / 16 + 1.
-inline int pack_pages(int n) { return (n + 28) / kPage + 2; }
 
 // The offset-binary codes q + 8 of the 8 bf16 elements of x under scale s
 // (inv ~ 1 / s), the rule of quant_code, with code u in the low byte of b[u]

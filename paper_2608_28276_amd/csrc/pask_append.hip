@@ -1141,10 +1141,6 @@ hipError_t launch_append(const AppendArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-int64_t append_blocks(int32_t max_new, int32_t window) {
-  return std::max(pack_pages(max_new + window), std::min(max_new, window));
-}
-
 hipError_t launch_append_plan(const AppendArgs& a, hipStream_t s) {
   append_plan_kernel<false, false><<<dim3(a.batch), dim3(kPlanThreads), 0, s>>>(a);
   return hipGetLastError();

@@ -13,14 +13,9 @@
 #include <hip/hip_runtime_api.h>
 
 #include "pask_internal.h"
+#include "pask_pages.h"
 
 namespace pask {
-
-// Most workgroups (256 threads) of one sequence that a kernel of a bulk append
-// is launched with; a launch holds 2^32 - 1 threads, and one that fails after
-// the plan has counted the tokens leaves entries whose pages nobody wrote.
-int64_t append_blocks(int32_t max_new, int32_t window);
-inline bool append_fits(int32_t max_new, int32_t window) { return append_blocks(max_new, window) < 1 << 24; }
 
 constexpr uint64_t kAlignSmall = 256;
 constexpr uint64_t kAlignPool = 4096;
