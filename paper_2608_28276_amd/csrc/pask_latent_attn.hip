@@ -246,10 +246,13 @@ struct Tile {
 //   scores  S^T = C Q^T on v_mfma_f32_16x16x32_bf16, a wave per head tile (per
 //           page of a head tile, up to 32 heads): lane (q, n) holds head n's
 //           scores of slots 4q .. 4q + 3 of a page; queries stay in registers.
-//   weights online softmax in base 2.  Weights are rounded to bf16 (half a step,
-//           2^-8 of a weight; independent over slots, so it averages out below
-//           the output's own rounding); their sum is kept of the unrounded ones
-//           in fp32.  A head's reference moves only when a score exceeds it by
+//   weights online softmax in base 2.  Weights are rounded once to bf16 (half a
+//           step, 2^-8 of a weight), their sum is kept of the unrounded ones in
+//           fp32.  The rounding adds about as much to the output's error as the
+//           output's own: 2.2e-3 relative to the 64-bit result (64 sequences,
+//           16 heads), 1.7e-3 with weights of 32 bits.  The grouped-query kernel
+//           splits a HIGH page's weights in two; here that would double the
+//           value products and the weights' way through LDS.  A head's reference moves only when a score exceeds it by
 //           more than kHeadroom: weights up to 2^16 are as precise as those
 //           below 1, and the sums of values, which fill the registers, are left
 //           alone in the loop.
@@ -261,11 +264,13 @@ struct Tile {
 // buffers meanwhile, and the page ids of the one behind them into registers.
 // Up to 32 heads two workgroups of four waves share a compute unit, each with
 // one tile under way; more heads take eight waves' registers, and the one
-// workgroup keeps two tiles under way.  Few heads are bound by the memory (64
-// sequences of 1,000-8,192 tokens, 16 heads, rank 512: 192 MB in 53 us), many by
-// the chain copies - scores - values of a tile, the matrix cores being busy 35%
-// of the time (128 of 1,024-8,192, 128 heads: 157 GFLOP in 228 us, and 20 us for
-// the merge of 100 MB of partial results).  Scores of 32 heads by two waves that
+// workgroup keeps two tiles under way.  Few heads wait for their copies: 64
+// sequences of 1,000-8,192 tokens, 16 heads, rank 512 are 192 MB in 54 us, 3.6
+// TB/s where a plain read reaches 7.1, with 72 KiB under way per compute unit and
+// 6 us before the first product.  Many wait in the chain copies - scores - values
+// of a tile, the matrix cores being busy 35% of the time (128 of 1,024-8,192, 128
+// heads: 157 GFLOP in 225 us, and 20 us for the merge of 100 MB of partial
+// results); a LOW tile's widening is a link of that chain of its own.  Scores of 32 heads by two waves that
 // halve the dimensions and exchange sums halve the reads of keys from LDS and
 // took 24 us more.
 constexpr int latent_waves(int head_tiles) { return head_tiles >= 4 ? 8 : 4; }
@@ -612,8 +617,8 @@ __global__ __launch_bounds__(64 * latent_waves(NHT), 2) void latent_attn_kernel(
 // the first slots of the workers after it).  Up to 8 partials: a wave per head.
 // More: a workgroup per slice of a head, R / (8 slices) lanes to a partial, as
 // many partials at a time as fit, added up through LDS.  With few heads in the
-// call a head is cut into slices, down to 64 elements (275 partials of 20 heads:
-// 12 us whole, 6.7 in 8 slices); with enough to fill the chip it is not (64
+// call a head is cut into slices, down to 64 elements (376 partials of 20 heads:
+// 17 us whole, 8.5 in 8 slices); with enough to fill the chip it is not (64
 // sequences of 16 heads: 6.6 us whole, 12 in slices, each of which finds the
 // maximum again).
 template <int R>

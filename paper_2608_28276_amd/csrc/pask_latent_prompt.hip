@@ -81,8 +81,10 @@ __device__ __forceinline__ void add_seen_values(const uint8_t* s_v, f32x16_t s, 
 // the keys they see, 64 at a step, 32 at a time:
 //   scores  S^T = K Q^T on v_mfma_f32_32x32x16_bf16: a lane holds scores of one
 //           query, so its softmax needs one exchange (with the lane 32 on);
-//   weights online softmax in base 2, rounded to bf16 (2^-8 of a weight at
-//           most, as the values' own); sums are kept of the unrounded weights;
+//   weights online softmax in base 2, rounded once to bf16 (half a step, 2^-8
+//           of a weight; 2.1e-3 relative to the 64-bit result for the call
+//           below, 1.6e-3 with weights of 32 bits); sums are kept of the
+//           unrounded weights;
 //   values  O^T += V^T P^T: the scores' lane layout is the operand layout of P
 //           up to the order of the 16 keys of a product, which the value operand
 //           follows (two transposing reads of 4 keys).
@@ -94,9 +96,11 @@ __device__ __forceinline__ void add_seen_values(const uint8_t* s_v, f32x16_t s, 
 // from the end allows or, where the keys come with positions, as lie at its
 // position or before (8,192 queries and keys of 32 heads: 699 us by place, 710
 // by position).
-// Bound by the matrix cores and the exponentials beside them: 8,192 queries and
-// keys, 32 heads of 128 + 64 and values of 128 take 697-743 us from card to card
-// (687 GFLOP, 925-986 TFLOP/s); this loop's products alone take 516.
+// 8,192 queries and keys, 32 heads of 128 + 64 and values of 128 take 688-743 us
+// from card to card (687 GFLOP, 925-999 TFLOP/s); this loop's products alone take
+// 516.  Of what is between, most is the operands' reads from LDS, 1.45
+// instructions a product since each serves 32 queries of one wave: with operands
+// made in registers 583 us in place of 700.  Without exponentials it is 670.
 template <int N, int P, int V, int W>
 __global__ __launch_bounds__(64 * W, 2) void latent_prompt_kernel(LatentPromptArgs a, int q_tiles) {
   constexpr int T = 64 * W, kRows = 32 * W;

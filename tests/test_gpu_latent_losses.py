@@ -87,7 +87,7 @@ def test_a_full_sequence(kind):
 
 @pytest.mark.parametrize("kind", ["bulk", "one", "step"])
 def test_a_tag_outside_the_table(kind):
-    """Kept HIGH as a forced entry, and flagged; a call that keeps all does not look at tags."""
+    """Kept HIGH as a forced entry, and flagged."""
     p = Pair(batch=2, heads=5, rank=128, rope=32, action=[LOW, DROP], floor=[DROP, DROP], seed=10)
     p.append([5, 6])
     assert p.sess.stats()[1] == pask.PASK_OK
