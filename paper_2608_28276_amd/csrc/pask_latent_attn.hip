@@ -252,10 +252,10 @@ struct Tile {
 //           output's own: 2.2e-3 relative to the 64-bit result (64 sequences,
 //           16 heads), 1.7e-3 with weights of 32 bits.  The grouped-query kernel
 //           splits a HIGH page's weights in two; here that would double the
-//           value products and the weights' way through LDS.  A head's reference moves only when a score exceeds it by
-//           more than kHeadroom: weights up to 2^16 are as precise as those
-//           below 1, and the sums of values, which fill the registers, are left
-//           alone in the loop.
+//           value products and the weights' way through LDS.  A head's
+//           reference moves only when a score exceeds it by more than kHeadroom:
+//           weights up to 2^16 are as precise as those below 1, and the sums of
+//           values, which fill the registers, are left alone in the loop.
 //   values  O^T += C^T P^T: wave w of W owns output elements [w R / W, (w + 1) R
 //           / W) of every head, so a value is read from LDS once per workgroup;
 //           weights pass through LDS in the operand order (a score lane holds
@@ -270,9 +270,9 @@ struct Tile {
 // 6 us before the first product.  Many wait in the chain copies - scores - values
 // of a tile, the matrix cores being busy 35% of the time (128 of 1,024-8,192, 128
 // heads: 157 GFLOP in 225 us, and 20 us for the merge of 100 MB of partial
-// results); a LOW tile's widening is a link of that chain of its own.  Scores of 32 heads by two waves that
-// halve the dimensions and exchange sums halve the reads of keys from LDS and
-// took 24 us more.
+// results); a LOW tile's widening is a link of that chain of its own.
+// Scores of 32 heads by two waves that halve the dimensions and exchange sums
+// halve the reads of keys from LDS and took 24 us more.
 constexpr int latent_waves(int head_tiles) { return head_tiles >= 4 ? 8 : 4; }
 constexpr int latent_ahead(int head_tiles) { return head_tiles >= 4 ? 2 : 1; }
 constexpr float kHeadroom = 16.0f;

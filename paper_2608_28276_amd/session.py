@@ -370,7 +370,7 @@ class PaskLatentSession:
         """Back to a state that save() returned, on the same stream, as often as wanted.  Going back voids the states
         saved after it (their pages are handed out again), and a reset() all of them: a void state, or another
         session's, raises PaskError.  The check is made when restore() is called, not when a graph that captured it is
-        replayed: replay it only while the state is valid."""
+        replayed: replay it only while the state is valid, and hold on to the state as to a captured call's tensors."""
         if getattr(saved, "_key", None) is not self._key or (saved._captured and not self._capturing()):
             raise pask.PaskError(pask.PASK_E_ARG, "restore: not a state of this session, or void")
         if self._newest > saved._serial:
