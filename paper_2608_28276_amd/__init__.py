@@ -7,4 +7,4 @@ with torch and drives the ABI for a batch of sequences (`PaskSession`,
 `PaskLatentSession`).
 """
 
-__all__ = ["pask", "latent", "session"]
+__all__ = ["pask", "latent", "prompt", "session"]

@@ -23,10 +23,11 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libpask.so")
-# Persisting entries and reading them; the same for latents, absorbed and expanded attention.
+# Persisting entries and reading them; the same for latents, absorbed and expanded attention; rotary positions and the
+# attention of prompts over the mixed cache.
 KERNEL_SOURCES = ("pask_append.hip", "pask_attn.hip", "pask_latent.hip", "pask_latent_attn.hip",
-                  "pask_latent_prompt.hip")
-HOST_SOURCES = ("pask_api.cpp", "pask_latent_api.cpp")
+                  "pask_latent_prompt.hip", "pask_rope.hip", "pask_prompt.hip")
+HOST_SOURCES = ("pask_api.cpp", "pask_latent_api.cpp", "pask_prompt_api.cpp")
 # The benchmark's on-device bandwidth probes: a library of their own, outside the C ABI.
 PROBE_LIB = os.path.join(PKG, "libpask_probe.so")
 

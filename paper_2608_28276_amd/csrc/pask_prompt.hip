@@ -1,0 +1,691 @@
+// gfx950 kernels of the attention of many query tokens over the mixed cache:
+// bf16 pages, int4 pages and the recent window, causal by position, keys cut
+// into pieces where there are few queries.
+#include <hip/hip_runtime.h>
+
+#include <math.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "pask_latent_device.h"
+#include "pask_prompt_internal.h"
+
+namespace pask {
+namespace {
+
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+
+constexpr int kStepKeys = 64, kStepPages = kStepKeys / kPage;
+// The reference of a row's weights lies kBelow under a maximum (in base 2) and
+// moves only when a score exceeds it by more than kHeadroom: weights stay below
+// 2^15, which fp16 holds, and the largest is 2^8 or more, so that what fp16
+// cannot tell from 0 is 2^-33 of it.  bf16 and fp32 are as precise there as
+// below 1, and the sums stay below the largest fp32 for values that sum to less
+// than 2^112, the bound that the header gives.
+constexpr float kHeadroom = 15.0f, kBelow = 8.0f;
+constexpr int kAhead = 4;                          // score operands read ahead of their product
+constexpr float kLn2 = 0.6931471805599453f;
+
+// D[32x32] += A[32x16] B[16x32]: lane l holds A[l % 32][8 (l / 32) ..], B[8 (l / 32) ..][l % 32], and
+// D[8 (r / 4) + 4 (l / 32) + r % 4][l % 32], r < 16.
+__device__ __forceinline__ f32x16_t mfma(uint4 a, uint4 b, f32x16_t c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0,
+                                                 0, 0);
+}
+__device__ __forceinline__ f32x16_t mfma_half(uint4 a, uint4 b, f32x16_t c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0,
+                                                0);
+}
+__device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {   // round to nearest even
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t){lo, hi}, f16x2_t));
+}
+
+// The kinds of pages a sequence's keys come from, in the order they are taken.
+enum Kind { kLowPages = 0, kHighPages = 1, kWindowPages = 2 };
+
+// What the keys of one (sequence, layer) are, seen from queries at positions.
+struct Keys {
+  const int32_t* list[2];                          // positions of the LOW and HIGH entries, ascending
+  const int32_t* table[2];                         // their pages
+  int n[2];                                        // entries
+  int n_pos, ring_slots, ring_turn;                // positions; slots of the window in use; slot of the next position
+  int ring_page;                                   // first page of the window
+};
+
+__device__ __forceinline__ Keys keys_of(const CacheView& cv, int b, int layer) {
+  Keys k;
+  const int32_t* cnt = counters_of(cv, b, layer);
+  k.list[kLowPages] = index_list_of(cv, b, layer, kLo);
+  k.list[kHighPages] = index_list_of(cv, b, layer, kHi);
+  k.table[kLowPages] = block_table_of(cv, b, layer, kLo);
+  k.table[kHighPages] = block_table_of(cv, b, layer, kHi);
+  k.n[kLowPages] = cnt[kCntLo];
+  k.n[kHighPages] = cnt[kCntHi];
+  k.n_pos = cnt[kCntPos];
+  k.ring_slots = min(k.n_pos, cv.window);
+  k.ring_turn = cv.window ? k.n_pos % cv.window : 0;
+  k.ring_page = (int)sl_index(cv, b, layer) * cv.ring_pp;
+  return k;
+}
+// Position held by slot s of the window; INT64_MAX for a slot not in use.
+__device__ __forceinline__ long long ring_position(const Keys& k, int window, int s) {
+  if (s >= k.ring_slots) return INT64_MAX;
+  return (long long)k.n_pos - k.ring_turn + s - (s < k.ring_turn ? 0 : window);
+}
+// Entries of a list at position p or before.  An entry is one position, so no
+// more than the positions behind p lie behind it, and no more than p + 1 before.
+__device__ __forceinline__ int entries_at(const int32_t* list, int n, int n_pos, long long p) {
+  if (p >= n_pos - 1) return n;
+  if (p < 0) return 0;
+  const int x = (int)p + 1;
+  return entries_below(list, max(0, n - (n_pos - x)), min(n, x), x);
+}
+
+// Code j of a word times its scale s, exact in fp32 (a code has 3 bits, a scale 11).  Codes in byte order: the low
+// nibbles of bytes 0..3, then the high ones (LOW keys: 8 elements of a chunk; LOW values: 4 slots of one dimension,
+// then of the one 16 on).
+__device__ __forceinline__ float code_value(uint32_t w, int j, float s) {
+  const uint32_t n = j < 4 ? (w >> (8 * j)) & 15u : (w >> (8 * (j - 4) + 4)) & 15u;
+  return fmaf((float)n, s, -8.0f * s);
+}
+// The high halves of two fp32 as a pair of bf16 (their upper 8 significant bits), and what is left of them, at most 6
+// bits, as another: together the two fp32, where they have 14 bits.
+__device__ __forceinline__ uint32_t split_pair(float x, float y, uint32_t& rest) {
+  const uint32_t a = __float_as_uint(x), b = __float_as_uint(y);
+  const uint32_t r = __float_as_uint(x - __uint_as_float(a & 0xFFFF0000u));
+  const uint32_t q = __float_as_uint(y - __uint_as_float(b & 0xFFFF0000u));
+  rest = __builtin_amdgcn_perm(q, r, 0x07060302u);
+  return __builtin_amdgcn_perm(b, a, 0x07060302u);
+}
+
+// Codes and scales of one thread's share of a LOW page: quarter q of slot t's
+// key (NG words of 8 elements, slot t's NG scales), or 4 slots of NG pairs of
+// dimensions (e + 32 i, + 16) of the values (4 slots' NG scales).
+template <int D>
+struct LowPart {
+  static constexpr int NG = PageLayout<D>::NG;
+  uint32_t code[NG];
+  uint32_t scale[2 * NG];                          // keys: the first NG / 2
+};
+// A page with a scale above this holds values that fp16 does not; it is taken at 1 / 16 of them.
+constexpr float kWideScale = 65504.0f / 7.0f, kWide = 16.0f;
+
+// O += P V key by key over 32 keys (values of 2 pages at s_v), where a value
+// that some query does not see is infinite or NaN (a weight of 0 times it is
+// not 0): only what a query sees is added.  Lane (g, n) holds the weights of
+// query n for half of the keys, and which of them are hidden; lane (1 - g, n)
+// the others'.
+template <int VT, int kTile>
+__device__ __forceinline__ void add_seen_values(const uint8_t* s_v, f32x16_t s, uint32_t hidden, f32x16_t (&o)[VT], int g,
+                                                int n) {
+#pragma unroll 1
+  for (int x = 0; x < 16; ++x) {
+    asm volatile("" : "+v"(g));                    // no code: keeps this rare path's addresses out of the loops around it
+    const float mine = s[0];
+#pragma unroll
+    for (int r = 0; r < 15; ++r) s[r] = s[r + 1];
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      const float p = __shfl(mine, n + 32 * w);
+      const bool skip = (__shfl(hidden, n + 32 * w) >> x & 1u) != 0u;
+      const int t = 8 * (x >> 2) + 4 * w + (x & 3);
+      if (skip) continue;
+#pragma unroll
+      for (int m = 0; m < VT; ++m)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {             // element 32 m + d
+          const int d = 8 * (r >> 2) + 4 * g + (r & 3);
+          const uint8_t* at = s_v + (t >> 4) * kTile + m * 1024 + ((t & 15) >> 2) * 256 + (d & 15) * 16 + (d >> 4) * 8 +
+                              (t & 3) * 2;
+          o[m][r] += p * bf16_lo(*reinterpret_cast<const uint16_t*>(at));
+        }
+    }
+  }
+}
+
+// A workgroup of W waves takes 32 W rows of one KV head, row x being head x % G
+// of the group's G at query token x / G, through the keys that the tile sees,
+// 64 at a step, 32 at a time:
+//   scores  S^T = K Q^T on v_mfma_f32_32x32x16_bf16: a lane holds scores of one
+//           row, so its softmax needs one exchange (with the lane 32 on);
+//   weights online softmax in base 2, rounded once to the type of the values
+//           (bf16: half a step, 2^-8 of a weight); sums are kept of the
+//           unrounded weights;
+//   values  O^T += V^T P^T.
+// Pages lie in the order of 16-row operands; the operands of 32 rows are the
+// same 16-byte chunks of two pages (keys), and 8-byte halves of them (values:
+// the scores' lane layout is the operand layout of P up to the order of the 16
+// slots of a page, which two halves 512 bytes apart follow).  So HIGH pages go
+// to LDS as they lie, and every operand read is contiguous.
+// LOW pages are widened on the way, once for all rows of the workgroup: a key,
+// code times scale with up to 14 bits, as the sum of two bf16 (exact; its
+// scores take twice the products, half as many again in all), a value rounded
+// once to fp16 (half a step, 2^-11), with weights of fp16.  Keys of one bf16
+// made the outputs of int4 histories 3.4e-3 of their size wrong and lse 3e-5;
+// outputs of bf16 pages are 2.1e-3 wrong, most of it their own rounding.
+// The scores of the next 32 keys are computed beside the weights of the current
+// ones; two steps are on their way into a ring of three LDS buffers meanwhile.
+// The keys that a row sees are, in each store, those up to a place of its list;
+// in the window, a ring, those whose position is not behind the row's.
+template <int D, int G, int W>
+__global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a, int q_tiles) {
+  using L = PageLayout<D>;
+  constexpr int kRows = 32 * W, VT = D / 32, KI = D / 16, NG = L::NG;
+  // A page in LDS: keys, the rest of LOW keys, values.
+  constexpr int kPart = L::kHiV, kValues = 2 * kPart, kTile = 3 * kPart, kStep = kStepPages * kTile;
+  __shared__ __align__(1024) uint8_t s_kv[3][kStep];
+  __shared__ uint32_t s_wide[3][kStepPages];       // LOW pages whose values are at 1 / 16
+  const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int g = lane >> 5, n = lane & 31;
+  // Workgroups go to the 8 XCDs in turn: neighbours are different KV heads.  The longest tiles first.
+  int rest = (int)blockIdx.x;
+  const int head = rest % a.cv.n_kv_heads;
+  rest /= a.cv.n_kv_heads;
+  const int piece = rest % a.pieces;
+  rest /= a.pieces;
+  const int b = rest % a.batch, tile = q_tiles - 1 - rest / a.batch;
+  const int nq = a.n_q ? min(max(a.n_q[b], 0), a.max_q) : a.max_q;
+  const int n_rows = nq * G, tile0 = tile * kRows;
+  if (tile0 >= n_rows) return;
+  const Keys keys = keys_of(a.cv, b, a.layer);
+  const long long first = a.first ? (long long)a.first[b] : (long long)keys.n_pos - nq;
+  const int row0 = tile0 + wave * 32, row = row0 + n;
+  const bool in = row < n_rows;
+  // Entries of each list that the tile's last row, the wave's first and its last see, found by 16 lanes each.
+  const long long tile_at = first + (min(tile0 + kRows, n_rows) - 1) / G, wave_at = first + row0 / G;
+  const long long wave_end = first + (min(row0 + 32, n_rows) - 1) / G;
+  int n_see[2], first_sees[2], last_sees[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int seen = entries_at(keys.list[k], keys.n[k], keys.n_pos, lane < 16 ? tile_at : lane < 32 ? wave_at : wave_end);
+    n_see[k] = __builtin_amdgcn_readlane(seen, 0);
+    first_sees[k] = row0 < n_rows ? __builtin_amdgcn_readlane(seen, 16) : 0;
+    last_sees[k] = row0 < n_rows ? __builtin_amdgcn_readlane(seen, 32) : 0;
+  }
+  const bool ring_seen = keys.ring_slots > 0 && tile_at >= (long long)keys.n_pos - keys.ring_slots;
+  const int low_steps = (n_see[kLowPages] + kStepKeys - 1) / kStepKeys;
+  const int high_steps = (n_see[kHighPages] + kStepKeys - 1) / kStepKeys;
+  const int ring_steps = ring_seen ? (keys.ring_slots + kStepKeys - 1) / kStepKeys : 0;
+  const int steps = low_steps + high_steps + ring_steps;
+  const int j_begin = (int)((long long)steps * piece / a.pieces), j_end = (int)((long long)steps * (piece + 1) / a.pieces);
+
+  // Scores are scaled by |scale|; its sign goes to the queries, so that a score's maximum is a scaled one's.
+  uint4 qf[KI];
+  const uint32_t flip = a.scale_log2 < 0.0f ? 0x80008000u : 0u;
+  const float scale = fabsf(a.scale_log2);
+  const size_t q_row = (((size_t)b * a.max_q + (in ? row / G : 0)) * a.n_q_heads + (size_t)head * G + (in ? row % G : 0));
+  const uint16_t* qrow = a.q + q_row * D + 8 * g;
+#pragma unroll
+  for (int i = 0; i < KI; ++i) {
+    qf[i] = in ? *reinterpret_cast<const uint4*>(qrow + 16 * i) : make_uint4(0u, 0u, 0u, 0u);
+    qf[i] = make_uint4(qf[i].x ^ flip, qf[i].y ^ flip, qf[i].z ^ flip, qf[i].w ^ flip);
+  }
+
+  // Page ids, 64 of a kind's at a time, one per lane.
+  int ids = 0, ids_of = -1;                        // ids_of: kind and block of 64 pages that are held
+  auto page_at = [&](int kind, int p) {            // p: the same for the wave
+    if (kind == kWindowPages) return keys.ring_page + min(p, a.cv.ring_pp - 1);
+    const int of = (p >> 6) * 2 + kind;
+    if (of != ids_of) {
+      const int last = ((kind == kLowPages ? n_see[0] : n_see[1]) - 1) >> 4;   // missing pages repeat the last one
+      ids = (kind == kLowPages ? keys.table[0] : keys.table[1])[min((p & ~63) + lane, last)];
+      ids_of = of;
+    }
+    return __builtin_amdgcn_readlane(ids, p & 63);
+  };
+  auto head_slot = [&](int page) { return (int)(((unsigned)head + (unsigned)page) % (unsigned)a.cv.n_kv_heads); };
+  // The kind of the tile's step j and its first page.
+  auto kind_of = [&](int j) { return j < low_steps ? kLowPages : j < low_steps + high_steps ? kHighPages : kWindowPages; };
+  auto page0_of = [&](int j, int kind) {
+    return kStepPages * (j - (kind == kLowPages ? 0 : kind == kHighPages ? low_steps : low_steps + high_steps));
+  };
+  // A LOW step's parts of this wave: part x is the keys (x even) or values of page x / 2.
+  constexpr int kParts = (2 * kStepPages + W - 1) / W;
+  LowPart<D> low[kParts];
+  auto fetch = [&](int j) __attribute__((always_inline)) {
+    if (j >= j_end) return;
+    const int kind = kind_of(j), p0 = page0_of(j, kind);
+    if (kind == kLowPages) {
+#pragma unroll
+      for (int k = 0; k < kParts; ++k) {
+        const int x = wave + k * W;
+        const int page = page_at(kind, p0 + (x >> 1));
+        const uint8_t* src = a.cv.lo_pool + (size_t)page * a.cv.lo_page_bytes + (size_t)head_slot(page) * L::kLoHead;
+        const bool values = (x & 1) != 0;
+        const uint32_t* code = reinterpret_cast<const uint32_t*>(src + (values ? L::kLoVC : 0)) + lane * NG;
+        const uint32_t* scale_at = reinterpret_cast<const uint32_t*>(src + (values ? L::kLoVS : L::kLoKS));
+        scale_at += values ? (lane >> 4) * 2 * NG : (lane & 15) * (NG / 2);
+#pragma unroll
+        for (int i = 0; i < NG; ++i) low[k].code[i] = code[i];
+#pragma unroll
+        for (int i = 0; i < 2 * NG; ++i)
+          if (i < NG / 2 || values) low[k].scale[i] = scale_at[i];
+      }
+      return;
+    }
+    uint8_t* dst = s_kv[j % 3];
+    constexpr int kInstr = L::kHiHead / 1024;      // of a page
+#pragma unroll
+    for (int k = 0; k < (kStepPages * kInstr + W - 1) / W; ++k) {
+      const int x = wave + k * W, y = x % kInstr;
+      const int page = page_at(kind, p0 + x / kInstr);
+      const uint8_t* src = a.cv.hi_pool + (size_t)page * a.cv.hi_page_bytes + (size_t)head_slot(page) * L::kHiHead;
+      load_to_lds<false>(src + y * 1024 + lane * 16,
+                         dst + (x / kInstr) * kTile + y * 1024 + (y < kInstr / 2 ? 0 : kValues - kPart));
+    }
+  };
+  // A LOW step's arrived parts into its buffer, widened; slots behind the last entry as 0.
+  auto land = [&](int j) __attribute__((always_inline)) {
+    if (j >= j_end || kind_of(j) != kLowPages) return;
+    const uint32_t dst = lds_address(s_kv[j % 3]);
+#pragma unroll
+    for (int k = 0; k < kParts; ++k) {
+      const int x = wave + k * W, p = x >> 1;
+      const int slots = keys.n[kLowPages] - (page0_of(j, kLowPages) + p) * kPage;   // of the page in use
+      auto scale_of = [&](int t, int c) {          // slot t's, half c of the scales
+        const float s = half_value((uint16_t)(low[k].scale[c >> 1] >> (16 * (c & 1))));
+        return t < slots ? s : 0.0f;
+      };
+      if (x & 1) {
+        const uint32_t at = dst + p * kTile + kValues + lane * 16;
+        const int t0 = (lane >> 4) * 4;
+        bool wide = false;
+#pragma unroll
+        for (int c = 0; c < 4 * NG; ++c) wide |= scale_of(t0 + c / NG, c) > kWideScale;
+        const float unit = __ballot(wide) ? 1.0f / kWide : 1.0f;
+#pragma unroll
+        for (int i = 0; i < NG; ++i) {
+          float v[8];
+#pragma unroll
+          for (int t = 0; t < 8; ++t) v[t] = code_value(low[k].code[i], t, scale_of(t0 + t % 4, t % 4 * NG + i) * unit);
+          write_lds16(at + i * 1024, make_uint4(pack_half2(v[0], v[1]), pack_half2(v[2], v[3]), pack_half2(v[4], v[5]),
+                                                pack_half2(v[6], v[7])));
+        }
+        if (lane == 0) s_wide[j % 3][p] = unit != 1.0f;
+      } else {
+        const uint32_t at = dst + p * kTile + lane * 16;
+#pragma unroll
+        for (int i = 0; i < NG; ++i) {
+          const float s = scale_of(lane & 15, i);
+          uint4 hi, lo;
+          auto two = [&](int j, uint32_t& rest) {
+            return split_pair(code_value(low[k].code[i], j, s), code_value(low[k].code[i], j + 1, s), rest);
+          };
+          hi.x = two(0, lo.x);
+          hi.y = two(2, lo.y);
+          hi.z = two(4, lo.z);
+          hi.w = two(6, lo.w);
+          write_lds16(at + i * 1024, hi);
+          write_lds16(at + kPart + i * 1024, lo);
+        }
+      }
+    }
+  };
+
+  f32x16_t o[VT];
+#pragma unroll
+  for (int m = 0; m < VT; ++m)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[m][r] = 0.0f;
+  float mx = -INFINITY, sum = 0.0f;                // the reference (of scaled scores), the weights' sum
+  // Operand addresses in a unit of two pages: keys' chunk (2 i + g) of slot n, i < KI, at 512 i; values' halves of
+  // page h and dimensions 32 m .. at h * kTile + 1024 m, and 512 behind.
+  const uint32_t k_at = (uint32_t)((n >> 4) * kTile + g * 256 + (n & 15) * 16);
+  const uint32_t v_at = (uint32_t)(kValues + g * 256 + (n & 15) * 16 + (n >> 4) * 8);
+  auto unit_at = [&](int i) { return lds_address(s_kv[(i >> 1) % 3]) + (i & 1) * 2 * kTile; };
+  auto value_operand = [&](uint32_t vs, int h, int m) {
+    const uint32_t at = vs + h * kTile + m * 1024;
+    const u32x2_t x = *(const lds_u32x2*)(uintptr_t)at, y = *(const lds_u32x2*)(uintptr_t)(at + 512);
+    return make_uint4(x[0], x[1], y[0], y[1]);
+  };
+  // Products of a unit's scores and their operands: with LOW keys each part of the queries meets both of the key.
+  auto products = [](auto is_low) { return decltype(is_low)::value ? 2 * KI : KI; };
+  auto key_operand = [&](auto is_low, uint32_t ks, int k) {
+    return read_lds16(decltype(is_low)::value ? ks + 512 * (k >> 1) + (k & 1) * kPart : ks + 512 * k);
+  };
+  auto query_operand = [&](auto is_low, int k) { return qf[decltype(is_low)::value ? k >> 1 : k]; };
+  auto scores = [&](auto is_low, int i) __attribute__((always_inline)) {
+    f32x16_t s;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = 0.0f;
+    const uint32_t ks = fresh(unit_at(i) + k_at);
+#pragma unroll
+    for (int k = 0; k < products(is_low); ++k) s = mfma(key_operand(is_low, ks, k), query_operand(is_low, k), s);
+    return s;
+  };
+  auto highest = [&](const f32x16_t& s) {          // of the lane's row, scaled
+    float top = fmaxf(s[0], s[1]);
+#pragma unroll
+    for (int r = 2; r < 16; ++r) top = fmaxf(top, s[r]);
+    top = fmaxf(top, __shfl_xor(top, 32));
+    return top == -INFINITY ? top : top * scale;
+  };
+  auto exceeds = [&](float top) { return __ballot(top > mx + kHeadroom) != 0ull; };
+  auto refer = [&](float top) __attribute__((always_inline)) {                    // the reference follows a maximum that exceeds it
+    const float ref = top > mx + kHeadroom ? top - kBelow : mx;
+    const float alpha = ref == mx ? 1.0f : __builtin_amdgcn_exp2f(mx - ref);
+    sum *= alpha;
+#pragma unroll
+    for (int m = 0; m < VT; ++m) o[m] *= alpha;
+    mx = ref;
+  };
+  auto packed = [](auto is_low, const f32x16_t& s, int h) {   // weights of a page's 16 slots as an operand
+    auto two = [&](int r) {
+      return decltype(is_low)::value ? pack_half2(s[8 * h + r], s[8 * h + r + 1]) : pack_bf16x2(s[8 * h + r], s[8 * h + r + 1]);
+    };
+    return make_uint4(two(0), two(2), two(4), two(6));
+  };
+  auto add_values = [&](auto is_low, int i, const f32x16_t& s) __attribute__((always_inline)) {
+    const uint32_t vs = fresh(unit_at(i) + v_at);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint4 p = packed(is_low, s, h);
+#pragma unroll
+      for (int m = 0; m < VT; ++m)
+        o[m] = decltype(is_low)::value ? mfma_half(value_operand(vs, h, m), p, o[m]) : mfma(value_operand(vs, h, m), p, o[m]);
+    }
+  };
+  // A unit with pages at 1 / 16 of their values, and its values.
+  auto wide = [&](int i) {
+    const uint32_t* w = &s_wide[(i >> 1) % 3][2 * (i & 1)];
+    return __builtin_amdgcn_readfirstlane((int)(w[0] | w[1])) != 0;
+  };
+  auto add_wide = [&](int i, const f32x16_t& s) __attribute__((always_inline)) {
+    const uint32_t vs = fresh(unit_at(i) + v_at);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const float unit = s_wide[(i >> 1) % 3][2 * (i & 1) + h] ? kWide : 1.0f;
+      const uint4 p = packed(std::true_type{}, s, h);
+#pragma unroll
+      for (int m = 0; m < VT; ++m) {
+        o[m] *= 1.0f / unit;
+        o[m] = mfma_half(value_operand(vs, h, m), p, o[m]);
+        o[m] *= unit;
+      }
+    }
+  };
+
+  // Units of 32 keys.  After a step's first unit the workgroup meets: the next
+  // step has arrived (a LOW one is widened into its buffer), and the buffer of
+  // the step before is free for the step after next.
+  auto meet = [&](int i) __attribute__((always_inline)) {
+    if (i & 1) return;
+    wait_loads();
+    land(i / 2 + 1);
+    __syncthreads();
+    fetch(i / 2 + 2);
+  };
+  if (j_begin < j_end) {
+    fetch(j_begin);
+    wait_loads();
+    land(j_begin);
+    __syncthreads();
+    fetch(j_begin + 1);
+  }
+  // Unit i's scores s become weights beside the scores of unit i + 1.
+  float base = 0.0f, odd_sum = 0.0f, top = -INFINITY;
+  auto turn = [&](auto is_low, int i, f32x16_t& s, f32x16_t& next) __attribute__((always_inline)) {
+    constexpr int kProducts = decltype(is_low)::value ? 2 * KI : KI;
+    const uint32_t ks = fresh(unit_at(i + 1) + k_at);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) next[r] = 0.0f;
+    uint4 kf[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) kf[k] = key_operand(is_low, ks, k);
+    // Pinned order: a score product, the read of one to come, a part of the weights.
+#pragma unroll
+    for (int k = 0; k < kProducts; ++k) {
+      next = mfma(kf[k % kAhead], query_operand(is_low, k), next);
+      if (k + kAhead < kProducts) kf[k % kAhead] = key_operand(is_low, ks, k + kAhead);
+#pragma unroll
+      for (int r = 16 * k / kProducts; r < 16 * (k + 1) / kProducts; ++r) {
+        s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale, -base));
+        if (r & 1) odd_sum += s[r];
+        else sum += s[r];
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    add_values(is_low, i, s);
+    top = highest(next);
+    const bool leave = exceeds(top) || (decltype(is_low)::value && wide(i + 1));
+    meet(i);
+    return leave;
+  };
+  int i = 2 * j_begin;
+  // The units of one kind up to u1; u0: its first.  fs, ls: entries that the wave's first and last row see.
+  auto segment = [&](auto is_low, bool ring, int u0, int u1, int fs, int ls, const int32_t* list, int used) __attribute__((always_inline)) {
+    f32x16_t s;
+    // The units that all rows of the wave see whole.  The loop is left to move
+    // the reference, and for good at a wide unit, which the loop behind it takes.
+    int whole = min(u1, u0 + fs / 32);
+    auto stop_if_wide = [&] {
+      if (decltype(is_low)::value && i < whole && wide(i)) whole = i;
+    };
+    stop_if_wide();
+    if (i < whole) {
+      s = scores(is_low, i);
+      refer(highest(s));
+    }
+    while (i < whole) {
+      base = mx == -INFINITY ? 0.0f : mx;
+      f32x16_t t;
+      bool out = false;
+      while (i + 2 < whole) {                      // two turns, so that neither's scores are copied
+        out = turn(is_low, i, s, t);
+        ++i;
+        if (out) {
+          s = t;
+          break;
+        }
+        out = turn(is_low, i, t, s);
+        ++i;
+        if (out) break;
+      }
+      if (!out && i + 1 < whole) {
+        out = turn(is_low, i, s, t);
+        ++i;
+        s = t;
+      }
+      sum += odd_sum;
+      odd_sum = 0.0f;
+      if (out) {
+        refer(top);
+        stop_if_wide();
+      } else {                                     // the last of them
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale, -base));
+          sum += s[r];
+        }
+        add_values(is_low, i, s);
+        meet(i);
+        ++i;
+      }
+    }
+    // Units at the edge: some row of the wave does not see all their keys.  The
+    // entries between what the wave's first and last row see are fewer than its
+    // tokens: one per lane, counted for each token.
+    if (i >= u1) return;
+    const long long at = first + (in ? row / G : 0);
+    int sees = fs;
+    if (ls > fs) {
+      const int pos = lane < ls - fs ? list[fs + lane] : INT32_MAX;
+#pragma unroll 1
+      for (int x = 0; x < 32 / G; ++x) {
+        const int c = __popcll(__ballot(lane < ls - fs && (long long)pos <= wave_at + x));
+        if (at == wave_at + x) sees = fs + c;
+      }
+    }
+    if (!in) sees = 0;
+    for (; i < u1; ++i) {
+      const int slot0 = 32 * (i - u0);
+      if (row0 < n_rows && (ring || ls > slot0)) {
+        uint32_t hidden = 0u;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int slot = slot0 + 8 * (r >> 2) + 4 * g + (r & 3);
+          const bool hid = ring ? !in || ring_position(keys, a.cv.window, slot) > at : slot >= sees;
+          hidden |= (uint32_t)hid << r;
+        }
+        s = scores(is_low, i);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = hidden >> r & 1u ? -INFINITY : s[r];
+        refer(highest(s));
+        base = mx == -INFINITY ? 0.0f : mx;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const float w = __builtin_amdgcn_exp2f(fmaf(s[r], scale, -base));
+          s[r] = hidden >> r & 1u ? 0.0f : w;
+          sum += s[r];
+        }
+        if constexpr (decltype(is_low)::value) {
+          add_wide(i, s);
+        } else {
+          // Slots behind the last entry hold what was there before: taken as 0.
+          const int valid = used - slot0;
+          auto both = [&](int t) { return (t < valid ? 0xFFFFu : 0u) | (t + 1 < valid ? 0xFFFF0000u : 0u); };
+          const uint32_t vs = fresh(unit_at(i) + v_at);
+          auto operand = [&](int h, int m) {
+            const uint4 x = value_operand(vs, h, m);
+            const int t = 16 * h + 4 * g;
+            return make_uint4(x.x & both(t), x.y & both(t + 2), x.z & both(t + 8), x.w & both(t + 10));
+          };
+          bool wild = false;                       // some value is infinite or NaN
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int m = 0; m < VT; ++m) wild |= abs_max_bits8(operand(h, m)) >= 0x7F80u;
+          if (__ballot(wild)) {
+            add_seen_values<VT, kTile>(s_kv[(i >> 1) % 3] + (i & 1) * 2 * kTile + kValues, s, hidden, o, g, n);
+          } else {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const uint4 p = packed(is_low, s, h);
+#pragma unroll
+              for (int m = 0; m < VT; ++m) o[m] = mfma(operand(h, m), p, o[m]);
+            }
+          }
+        }
+      }
+      meet(i);
+    }
+  };
+  const int u_low = 2 * low_steps, u_high = 2 * (low_steps + high_steps), u_end = 2 * j_end;
+  if (i < min(u_low, u_end))
+    segment(std::true_type{}, false, 0, min(u_low, u_end), first_sees[0], last_sees[0], keys.list[0], keys.n[0]);
+#pragma unroll 1
+  for (int k = 0; k < 2; ++k) {                    // HIGH entries, then the window's
+    const int to = k ? u_end : min(u_high, u_end);
+    if (i >= to) continue;
+    segment(std::false_type{}, k == 1, k ? u_high : u_low, to, k ? 0 : first_sees[1], k ? 0 : last_sees[1], keys.list[1],
+            k ? keys.ring_slots : keys.n[1]);
+  }
+  sum += __shfl_xor(sum, 32);
+  if (!in) return;
+  if (a.pieces > 1) {
+    const size_t at = (((size_t)b * a.cv.n_kv_heads + head) * a.pieces + piece) * ((size_t)a.max_q * G) + row;
+#pragma unroll
+    for (int m = 0; m < VT; ++m)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4)
+        *reinterpret_cast<float4*>(a.ws_o + at * D + 32 * m + 2 * r + 4 * g) =
+            make_float4(o[m][r], o[m][r + 1], o[m][r + 2], o[m][r + 3]);
+    if (g == 0) *reinterpret_cast<float2*>(a.ws_ml + 2 * at) = make_float2(mx, sum);
+    return;
+  }
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+#pragma unroll
+  for (int m = 0; m < VT; ++m)
+#pragma unroll
+    for (int r = 0; r < 16; r += 4)
+      *reinterpret_cast<uint2*>(a.out + q_row * D + 32 * m + 2 * r + 4 * g) =
+          make_uint2(pack_bf16x2(o[m][r] * inv, o[m][r + 1] * inv), pack_bf16x2(o[m][r + 2] * inv, o[m][r + 3] * inv));
+  if (a.lse && g == 0) a.lse[q_row] = sum == 0.0f ? -INFINITY : (mx + __builtin_amdgcn_logf(sum)) * kLn2;
+}
+
+// Joins the pieces of a row, one wave per row: the parts' sums and outputs,
+// taken to the largest of their references.
+template <int D, int G>
+__global__ __launch_bounds__(256) void prompt_merge_kernel(PromptArgs a) {
+  const int lane = (int)threadIdx.x & 63;
+  const int64_t x = (int64_t)blockIdx.x * 4 + ((int)threadIdx.x >> 6), rows = (int64_t)a.max_q * G;
+  const int64_t bh = x / rows;
+  const int row = (int)(x - bh * rows), b = (int)(bh / a.cv.n_kv_heads), head = (int)(bh % a.cv.n_kv_heads);
+  if (b >= a.batch) return;
+  const int nq = a.n_q ? min(a.n_q[b], a.max_q) : a.max_q;
+  if (row >= nq * G) return;
+  const size_t first = (size_t)bh * a.pieces * rows + row;
+  float top = -INFINITY;
+  for (int p = 0; p < a.pieces; ++p) top = fmaxf(top, a.ws_ml[2 * (first + (size_t)p * rows)]);
+  float sum = 0.0f, o[D / 64];
+#pragma unroll
+  for (int d = 0; d < D / 64; ++d) o[d] = 0.0f;
+  for (int p = 0; p < a.pieces; ++p) {
+    const size_t at = first + (size_t)p * rows;
+    const float2 ml = *reinterpret_cast<const float2*>(a.ws_ml + 2 * at);
+    if (ml.y == 0.0f) continue;                    // a piece of which the row sees nothing
+    const float w = __builtin_amdgcn_exp2f(ml.x - top);
+    sum = fmaf(ml.y, w, sum);
+#pragma unroll
+    for (int d = 0; d < D / 64; ++d) o[d] = fmaf(a.ws_o[at * D + lane * (D / 64) + d], w, o[d]);
+  }
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+  const size_t to = ((size_t)b * a.max_q + row / G) * a.n_q_heads + (size_t)head * G + row % G;
+  if constexpr (D == 128) {
+    *reinterpret_cast<uint32_t*>(a.out + to * D + 2 * lane) = pack_bf16x2(o[0] * inv, o[1] * inv);
+  } else {
+    a.out[to * D + lane] = f32_to_bf16_rne_dev(o[0] * inv);
+  }
+  if (a.lse && lane == 0) a.lse[to] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+}
+
+template <int D, int G>
+void launch_group(const PromptArgs& a, const PromptCut& c, hipStream_t s) {
+  const dim3 blocks((unsigned)prompt_blocks(a, c));
+  const int q_tiles = (a.max_q * G + c.rows - 1) / c.rows;
+  prompt_kernel<D, G, 8><<<blocks, dim3(512), 0, s>>>(a, q_tiles);
+  if (a.pieces > 1) {
+    const int64_t rows = (int64_t)a.batch * a.cv.n_kv_heads * a.max_q * G;
+    prompt_merge_kernel<D, G><<<dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s>>>(a);
+  }
+}
+
+template <int D>
+void launch_dim(const PromptArgs& a, const PromptCut& c, hipStream_t s) {
+  switch (a.n_q_heads / a.cv.n_kv_heads) {
+    case 1: launch_group<D, 1>(a, c, s); break;
+    case 2: launch_group<D, 2>(a, c, s); break;
+    case 4: launch_group<D, 4>(a, c, s); break;
+    default: launch_group<D, 8>(a, c, s); break;
+  }
+}
+
+}  // namespace
+
+// Tiles of 256 rows (eight waves share every page through LDS).  The keys are
+// cut where the tiles leave compute units idle, into pieces of at least 256.
+PromptCut prompt_cut(int32_t batch, int32_t max_q, int32_t group, int32_t n_kv_heads, int32_t max_ctx_hint) {
+  PromptCut c;
+  const int64_t rows = (int64_t)max_q * group;
+  c.rows = 256;
+  const int64_t tiles = (rows + c.rows - 1) / c.rows * batch * n_kv_heads;
+  c.pieces = (int32_t)std::max<int64_t>(1, std::min<int64_t>(256 / tiles, (max_ctx_hint + 255) / 256));
+  return c;
+}
+
+int64_t prompt_blocks(const PromptArgs& a, const PromptCut& c) {
+  const int64_t rows = (int64_t)a.max_q * (a.n_q_heads / a.cv.n_kv_heads);
+  return (rows + c.rows - 1) / c.rows * a.batch * a.cv.n_kv_heads * a.pieces;
+}
+
+hipError_t launch_prompt(const PromptArgs& a, const PromptCut& c, hipStream_t s) {
+  if (a.cv.head_dim == 64) launch_dim<64>(a, c, s);
+  else launch_dim<128>(a, c, s);
+  return hipGetLastError();
+}
+
+}  // namespace pask

@@ -11,7 +11,7 @@ import weakref
 
 import torch
 
-from . import latent, pask
+from . import latent, pask, prompt
 
 # The current stream's raw handle: building torch's Stream object costs 2 us of
 # a call's 10.6.  Not in torch's public interface: a torch without it goes the
@@ -92,6 +92,50 @@ class PaskSession:
         hint = max_ctx_hint or self.max_ctx_hint
         pask.pask_decode_attn_noalloc(self.policy, self.cache, layer, b, q, out, lse, tags_new, k_new, v_new,
                                       self.softmax_scale, hint, self.stream, states_new=states_new)
+
+    def next_positions(self, layer: int, batch: int | None = None):
+        """int32 [batch], a copy: the position that the next token of each sequence takes in this layer."""
+        b = self.geom.max_batch if batch is None else batch
+        if not (0 <= layer < self.geom.n_layers and 1 <= b <= self.geom.max_batch):
+            raise pask.PaskError(pask.PASK_E_SHAPE, "next_positions: layer or batch out of range")
+        return self.counters()[:b, layer, 2].clone(memory_format=torch.contiguous_format)
+
+    def rotate(self, rope, layer: int, q, q_out, k=None, k_out=None, n_new=None):
+        """prompt.rotate at the positions that the next append() to this layer gives the rows, read from the cache's
+        counters when the kernel runs: before that append, on the same stream."""
+        g = self.geom
+        some = q if q is not None else k
+        if not isinstance(some, torch.Tensor) or not some.dim():
+            raise pask.PaskError(pask.PASK_E_ARG, "rotate: q or k expected")
+        if not (0 <= layer < g.n_layers and some.shape[0] <= g.max_batch):
+            raise pask.PaskError(pask.PASK_E_SHAPE, "rotate: layer or batch out of range")
+        stride = self.layout.counter_stride
+        prompt.rotate(rope, q, q_out, k, k_out, first=self.counters().view(-1)[layer * stride + 2:],
+                      first_stride=g.n_layers * stride, n_new=n_new)
+
+    def prompt(self, layer: int, q, out, lse=None, n_q=None, first=None, max_ctx_hint: int | None = None):
+        """Attention of many query tokens of each sequence over the persisted history (pask_prompt_attn): q, out bf16
+        [batch, max_q, Hq, D], lse fp32 [batch, max_q, Hq] or None.  n_q int32 [batch]: the queries of each sequence
+        (None: max_q).  first int32 [batch]: their first position; None: they are the last tokens appended.  Rows behind
+        n_q are left alone.  The workspace, where one is needed, is torch's for the length of the call."""
+        g, bf16 = self.geom, torch.bfloat16
+        buf = self.buf.device
+        latent.check_tensor("q", q, bf16, (None, None, g.n_q_heads, g.head_dim), buf)
+        b, m = q.shape[:2]
+        latent.check_tensor("out", out, bf16, (b, m, g.n_q_heads, g.head_dim), buf)
+        if lse is not None:
+            latent.check_tensor("lse", lse, torch.float32, (b, m, g.n_q_heads), buf)
+        for name, t in (("n_q", n_q), ("first", first)):
+            if t is not None:
+                latent.check_tensor(name, t, torch.int32, (b,), buf)
+        if m == 0:
+            return
+        hint = max_ctx_hint or self.max_ctx_hint
+        with torch.cuda.device(buf):
+            need = prompt.pask_prompt_workspace_bytes(g, b, m, hint)
+            ws = torch.empty(need, dtype=torch.uint8, device=buf) if need else None
+            prompt.pask_prompt_attn(self.cache, layer, b, m, n_q, first, q, out, lse, self.softmax_scale, hint, ws, need,
+                                    self.stream)
 
     def budgets(self):
         """Remaining budget R of every (sequence, layer), int64 [max_batch, n_layers]."""
