@@ -225,19 +225,26 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a, int
     qf[i] = make_uint4(qf[i].x ^ flip, qf[i].y ^ flip, qf[i].z ^ flip, qf[i].w ^ flip);
   }
 
-  // Page ids, 64 of a kind's at a time, one per lane.
-  int ids = 0, ids_of = -1;                        // ids_of: kind and block of 64 pages that are held
+  // Where the head's part of a page starts in its pool, 64 pages of a kind at a time, one per lane.
+  uint32_t from_lo = 0, from_hi = 0;
+  int from_of = -1;                                // kind and block of 64 pages that are held
   auto page_at = [&](int kind, int p) {            // p: the same for the wave
-    if (kind == kWindowPages) return keys.ring_page + min(p, a.cv.ring_pp - 1);
-    const int of = (p >> 6) * 2 + kind;
-    if (of != ids_of) {
-      const int last = ((kind == kLowPages ? n_see[0] : n_see[1]) - 1) >> 4;   // missing pages repeat the last one
-      ids = (kind == kLowPages ? keys.table[0] : keys.table[1])[min((p & ~63) + lane, last)];
-      ids_of = of;
+    const int of = (p >> 6) * 4 + kind;
+    if (of != from_of) {
+      const int at = (p & ~63) + lane;             // pages behind the last one repeat it
+      const int page = kind == kWindowPages ? keys.ring_page + min(at, a.cv.ring_pp - 1)
+                       : kind == kLowPages  ? keys.table[0][min(at, (n_see[0] - 1) >> 4)]
+                                            : keys.table[1][min(at, (n_see[1] - 1) >> 4)];
+      const uint32_t hs = ((uint32_t)head + (uint32_t)page) % (uint32_t)a.cv.n_kv_heads;
+      const uint64_t from = kind == kLowPages ? (uint64_t)page * a.cv.lo_page_bytes + hs * (uint32_t)L::kLoHead
+                                              : (uint64_t)page * a.cv.hi_page_bytes + hs * (uint32_t)L::kHiHead;
+      from_lo = (uint32_t)from;
+      from_hi = (uint32_t)(from >> 32);
+      from_of = of;
     }
-    return __builtin_amdgcn_readlane(ids, p & 63);
+    const uint32_t lo = __builtin_amdgcn_readlane(from_lo, p & 63), hi = __builtin_amdgcn_readlane(from_hi, p & 63);
+    return (kind == kLowPages ? a.cv.lo_pool : a.cv.hi_pool) + ((uint64_t)hi << 32 | lo);
   };
-  auto head_slot = [&](int page) { return (int)(((unsigned)head + (unsigned)page) % (unsigned)a.cv.n_kv_heads); };
   // The kind of the tile's step j and its first page.
   auto kind_of = [&](int j) { return j < low_steps ? kLowPages : j < low_steps + high_steps ? kHighPages : kWindowPages; };
   auto page0_of = [&](int j, int kind) {
@@ -246,15 +253,14 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a, int
   // A LOW step's parts of this wave: part x is the keys (x even) or values of page x / 2.
   constexpr int kParts = (2 * kStepPages + W - 1) / W;
   LowPart<D> low[kParts];
-  auto fetch = [&](int j) __attribute__((always_inline)) {
+  auto fetch = [&](auto low_too, int j) __attribute__((always_inline)) {
     if (j >= j_end) return;
     const int kind = kind_of(j), p0 = page0_of(j, kind);
-    if (kind == kLowPages) {
+    if (decltype(low_too)::value && kind == kLowPages) {
 #pragma unroll
       for (int k = 0; k < kParts; ++k) {
         const int x = wave + k * W;
-        const int page = page_at(kind, p0 + (x >> 1));
-        const uint8_t* src = a.cv.lo_pool + (size_t)page * a.cv.lo_page_bytes + (size_t)head_slot(page) * L::kLoHead;
+        const uint8_t* src = page_at(kind, p0 + (x >> 1));
         const bool values = (x & 1) != 0;
         const uint32_t* code = reinterpret_cast<const uint32_t*>(src + (values ? L::kLoVC : 0)) + lane * NG;
         const uint32_t* scale_at = reinterpret_cast<const uint32_t*>(src + (values ? L::kLoVS : L::kLoKS));
@@ -272,9 +278,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a, int
 #pragma unroll
     for (int k = 0; k < (kStepPages * kInstr + W - 1) / W; ++k) {
       const int x = wave + k * W, y = x % kInstr;
-      const int page = page_at(kind, p0 + x / kInstr);
-      const uint8_t* src = a.cv.hi_pool + (size_t)page * a.cv.hi_page_bytes + (size_t)head_slot(page) * L::kHiHead;
-      load_to_lds<false>(src + y * 1024 + lane * 16,
+      load_to_lds<false>(page_at(kind, p0 + x / kInstr) + y * 1024 + lane * 16,
                          dst + (x / kInstr) * kTile + y * 1024 + (y < kInstr / 2 ? 0 : kValues - kPart));
     }
   };
@@ -336,25 +340,34 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a, int
   // page h and dimensions 32 m .. at h * kTile + 1024 m, and 512 behind.
   const uint32_t k_at = (uint32_t)((n >> 4) * kTile + g * 256 + (n & 15) * 16);
   const uint32_t v_at = (uint32_t)(kValues + g * 256 + (n & 15) * 16 + (n >> 4) * 8);
-  auto unit_at = [&](int i) { return lds_address(s_kv[(i >> 1) % 3]) + (i & 1) * 2 * kTile; };
+  int slot = j_begin % 3;                          // buffer of the current unit's step
+  auto after = [](int s) { return s == 2 ? 0 : s + 1; };
+  auto unit_at = [&](int s, int i) { return lds_address(s_kv[0]) + s * kStep + (i & 1) * 2 * kTile; };
   auto value_operand = [&](uint32_t vs, int h, int m) {
     const uint32_t at = vs + h * kTile + m * 1024;
     const u32x2_t x = *(const lds_u32x2*)(uintptr_t)at, y = *(const lds_u32x2*)(uintptr_t)(at + 512);
     return make_uint4(x[0], x[1], y[0], y[1]);
   };
-  // Products of a unit's scores and their operands: with LOW keys each part of the queries meets both of the key.
-  auto products = [](auto is_low) { return decltype(is_low)::value ? 2 * KI : KI; };
+  // Operand k of a unit's scores: with LOW keys each part of the queries meets both of the key.
   auto key_operand = [&](auto is_low, uint32_t ks, int k) {
     return read_lds16(decltype(is_low)::value ? ks + 512 * (k >> 1) + (k & 1) * kPart : ks + 512 * k);
   };
   auto query_operand = [&](auto is_low, int k) { return qf[decltype(is_low)::value ? k >> 1 : k]; };
   auto scores = [&](auto is_low, int i) __attribute__((always_inline)) {
+    constexpr int kProducts = decltype(is_low)::value ? 2 * KI : KI;
     f32x16_t s;
 #pragma unroll
     for (int r = 0; r < 16; ++r) s[r] = 0.0f;
-    const uint32_t ks = fresh(unit_at(i) + k_at);
+    const uint32_t ks = fresh(unit_at(slot, i) + k_at);
+    uint4 ring[kAhead];
 #pragma unroll
-    for (int k = 0; k < products(is_low); ++k) s = mfma(key_operand(is_low, ks, k), query_operand(is_low, k), s);
+    for (int k = 0; k < kAhead; ++k) ring[k] = key_operand(is_low, ks, k);
+#pragma unroll
+    for (int k = 0; k < kProducts; ++k) {
+      s = mfma(ring[k % kAhead], query_operand(is_low, k), s);
+      if (k + kAhead < kProducts) ring[k % kAhead] = key_operand(is_low, ks, k + kAhead);
+      __builtin_amdgcn_sched_barrier(0);
+    }
     return s;
   };
   auto highest = [&](const f32x16_t& s) {          // of the lane's row, scaled
@@ -365,7 +378,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a, int
     return top == -INFINITY ? top : top * scale;
   };
   auto exceeds = [&](float top) { return __ballot(top > mx + kHeadroom) != 0ull; };
-  auto refer = [&](float top) __attribute__((always_inline)) {                    // the reference follows a maximum that exceeds it
+  auto refer = [&](float top) __attribute__((always_inline)) {   // the reference follows a maximum that exceeds it
     const float ref = top > mx + kHeadroom ? top - kBelow : mx;
     const float alpha = ref == mx ? 1.0f : __builtin_amdgcn_exp2f(mx - ref);
     sum *= alpha;
@@ -379,137 +392,73 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a, int
     };
     return make_uint4(two(0), two(2), two(4), two(6));
   };
-  auto add_values = [&](auto is_low, int i, const f32x16_t& s) __attribute__((always_inline)) {
-    const uint32_t vs = fresh(unit_at(i) + v_at);
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const uint4 p = packed(is_low, s, h);
-#pragma unroll
-      for (int m = 0; m < VT; ++m)
-        o[m] = decltype(is_low)::value ? mfma_half(value_operand(vs, h, m), p, o[m]) : mfma(value_operand(vs, h, m), p, o[m]);
-    }
+  auto add_product = [&](auto is_low, uint4 v, uint4 p, f32x16_t c) {
+    return decltype(is_low)::value ? mfma_half(v, p, c) : mfma(v, p, c);
   };
-  // A unit with pages at 1 / 16 of their values, and its values.
-  auto wide = [&](int i) {
-    const uint32_t* w = &s_wide[(i >> 1) % 3][2 * (i & 1)];
-    return __builtin_amdgcn_readfirstlane((int)(w[0] | w[1])) != 0;
-  };
-  auto add_wide = [&](int i, const f32x16_t& s) __attribute__((always_inline)) {
-    const uint32_t vs = fresh(unit_at(i) + v_at);
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const float unit = s_wide[(i >> 1) % 3][2 * (i & 1) + h] ? kWide : 1.0f;
-      const uint4 p = packed(std::true_type{}, s, h);
-#pragma unroll
-      for (int m = 0; m < VT; ++m) {
-        o[m] *= 1.0f / unit;
-        o[m] = mfma_half(value_operand(vs, h, m), p, o[m]);
-        o[m] *= unit;
-      }
-    }
+  // Pages of a step at 1 / 16 of their values.
+  auto any_wide = [&](int s) {
+    return __builtin_amdgcn_readfirstlane((int)(s_wide[s][0] | s_wide[s][1] | s_wide[s][2] | s_wide[s][3])) != 0;
   };
 
   // Units of 32 keys.  After a step's first unit the workgroup meets: the next
   // step has arrived (a LOW one is widened into its buffer), and the buffer of
   // the step before is free for the step after next.
-  auto meet = [&](int i) __attribute__((always_inline)) {
-    if (i & 1) return;
+  auto meet = [&](auto is_low, int j) __attribute__((always_inline)) {
     wait_loads();
-    land(i / 2 + 1);
+    if (decltype(is_low)::value) land(j + 1);      // LOW steps come first
     __syncthreads();
-    fetch(i / 2 + 2);
+    fetch(is_low, j + 2);
   };
   if (j_begin < j_end) {
-    fetch(j_begin);
+    fetch(std::true_type{}, j_begin);
     wait_loads();
     land(j_begin);
     __syncthreads();
-    fetch(j_begin + 1);
+    fetch(std::true_type{}, j_begin + 1);
   }
-  // Unit i's scores s become weights beside the scores of unit i + 1.
+  // Unit i's scores s become weights and add its values, beside the scores of unit i + 1.
   float base = 0.0f, odd_sum = 0.0f, top = -INFINITY;
-  auto turn = [&](auto is_low, int i, f32x16_t& s, f32x16_t& next) __attribute__((always_inline)) {
-    constexpr int kProducts = decltype(is_low)::value ? 2 * KI : KI;
-    const uint32_t ks = fresh(unit_at(i + 1) + k_at);
+  auto turn = [&](auto is_low, auto is_odd, int i, f32x16_t& s, f32x16_t& next) __attribute__((always_inline)) {
+    constexpr int kProducts = decltype(is_low)::value ? 2 * KI : KI, kAll = kProducts + 2 * VT;
+    constexpr bool kOdd = decltype(is_odd)::value;
+    const uint32_t ks = fresh(unit_at(kOdd ? after(slot) : slot, kOdd ? 0 : 1) + k_at);
+    const uint32_t vs = fresh(unit_at(slot, kOdd ? 1 : 0) + v_at);
+    auto operand = [&](int x) {
+      return x < kProducts ? key_operand(is_low, ks, x) : value_operand(vs, (x - kProducts) / VT, (x - kProducts) % VT);
+    };
 #pragma unroll
     for (int r = 0; r < 16; ++r) next[r] = 0.0f;
-    uint4 kf[kAhead];
+    uint4 ring[kAhead], p = make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) kf[k] = key_operand(is_low, ks, k);
-    // Pinned order: a score product, the read of one to come, a part of the weights.
+    for (int x = 0; x < kAhead; ++x) ring[x] = operand(x);
+    // Pinned order: a product, the read of an operand to come, a part of the weights.
 #pragma unroll
-    for (int k = 0; k < kProducts; ++k) {
-      next = mfma(kf[k % kAhead], query_operand(is_low, k), next);
-      if (k + kAhead < kProducts) kf[k % kAhead] = key_operand(is_low, ks, k + kAhead);
-#pragma unroll
-      for (int r = 16 * k / kProducts; r < 16 * (k + 1) / kProducts; ++r) {
-        s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale, -base));
-        if (r & 1) odd_sum += s[r];
-        else sum += s[r];
+    for (int x = 0; x < kAll; ++x) {
+      if (x >= kProducts && (x - kProducts) % VT == 0) p = packed(is_low, s, (x - kProducts) / VT);
+      if (x < kProducts) {
+        next = mfma(ring[x % kAhead], query_operand(is_low, x), next);
+      } else {
+        const int m = (x - kProducts) % VT;
+        o[m] = add_product(is_low, ring[x % kAhead], p, o[m]);
       }
+      if (x + kAhead < kAll) ring[x % kAhead] = operand(x + kAhead);
+      if (x < kProducts)
+#pragma unroll
+        for (int r = 16 * x / kProducts; r < 16 * (x + 1) / kProducts; ++r) {
+          s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale, -base));
+          if (r & 1) odd_sum += s[r];
+          else sum += s[r];
+        }
+      if (x == kProducts) top = highest(next);
       __builtin_amdgcn_sched_barrier(0);
     }
-    add_values(is_low, i, s);
-    top = highest(next);
-    const bool leave = exceeds(top) || (decltype(is_low)::value && wide(i + 1));
-    meet(i);
-    return leave;
   };
   int i = 2 * j_begin;
   // The units of one kind up to u1; u0: its first.  fs, ls: entries that the wave's first and last row see.
-  auto segment = [&](auto is_low, bool ring, int u0, int u1, int fs, int ls, const int32_t* list, int used) __attribute__((always_inline)) {
-    f32x16_t s;
-    // The units that all rows of the wave see whole.  The loop is left to move
-    // the reference, and for good at a wide unit, which the loop behind it takes.
-    int whole = min(u1, u0 + fs / 32);
-    auto stop_if_wide = [&] {
-      if (decltype(is_low)::value && i < whole && wide(i)) whole = i;
-    };
-    stop_if_wide();
-    if (i < whole) {
-      s = scores(is_low, i);
-      refer(highest(s));
-    }
-    while (i < whole) {
-      base = mx == -INFINITY ? 0.0f : mx;
-      f32x16_t t;
-      bool out = false;
-      while (i + 2 < whole) {                      // two turns, so that neither's scores are copied
-        out = turn(is_low, i, s, t);
-        ++i;
-        if (out) {
-          s = t;
-          break;
-        }
-        out = turn(is_low, i, t, s);
-        ++i;
-        if (out) break;
-      }
-      if (!out && i + 1 < whole) {
-        out = turn(is_low, i, s, t);
-        ++i;
-        s = t;
-      }
-      sum += odd_sum;
-      odd_sum = 0.0f;
-      if (out) {
-        refer(top);
-        stop_if_wide();
-      } else {                                     // the last of them
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale, -base));
-          sum += s[r];
-        }
-        add_values(is_low, i, s);
-        meet(i);
-        ++i;
-      }
-    }
-    // Units at the edge: some row of the wave does not see all their keys.  The
-    // entries between what the wave's first and last row see are fewer than its
-    // tokens: one per lane, counted for each token.
-    if (i >= u1) return;
+  auto segment = [&](auto is_low, bool ring, int u0, int u1, int fs, int ls, const int32_t* list, int used)
+      __attribute__((always_inline)) {
+    // The entries between what the wave's first and last row see are fewer than
+    // its tokens: one per lane, counted for each token.
     const long long at = first + (in ? row / G : 0);
     int sees = fs;
     if (ls > fs) {
@@ -521,14 +470,37 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a, int
       }
     }
     if (!in) sees = 0;
-    for (; i < u1; ++i) {
+    const int whole = min(u1, u0 + fs / 32);       // the units that all rows of the wave see whole
+    while (i < u1) {
+      f32x16_t s;
+      // Steps whose units are whole.  The loop is left to move the reference and at wide pages.
+      if (!(i & 1) && i + 1 < whole && !(decltype(is_low)::value && any_wide(slot))) {
+        f32x16_t t;
+        s = scores(is_low, i);
+        refer(highest(s));
+        base = mx;
+        for (;;) {
+          turn(is_low, std::false_type{}, i, s, t);
+          meet(is_low, i >> 1);
+          ++i;
+          if (exceeds(top)) break;
+          turn(is_low, std::true_type{}, i, t, s);
+          ++i;
+          slot = after(slot);
+          if (exceeds(top) || i + 1 >= whole || (decltype(is_low)::value && any_wide(slot))) break;
+        }
+        sum += odd_sum;
+        odd_sum = 0.0f;
+        if (i >= u1) break;
+      }
+      // One unit by itself, as at the edge: some row of the wave does not see all its keys.
       const int slot0 = 32 * (i - u0);
       if (row0 < n_rows && (ring || ls > slot0)) {
         uint32_t hidden = 0u;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          const int slot = slot0 + 8 * (r >> 2) + 4 * g + (r & 3);
-          const bool hid = ring ? !in || ring_position(keys, a.cv.window, slot) > at : slot >= sees;
+          const int k = slot0 + 8 * (r >> 2) + 4 * g + (r & 3);
+          const bool hid = ring ? !in || ring_position(keys, a.cv.window, k) > at : k >= sees;
           hidden |= (uint32_t)hid << r;
         }
         s = scores(is_low, i);
@@ -542,13 +514,24 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a, int
           s[r] = hidden >> r & 1u ? 0.0f : w;
           sum += s[r];
         }
+        const uint32_t vs = fresh(unit_at(slot, i) + v_at);
         if constexpr (decltype(is_low)::value) {
-          add_wide(i, s);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint4 p = packed(is_low, s, h);
+            const float unit = s_wide[slot][2 * (i & 1) + h] ? kWide : 1.0f;
+#pragma unroll
+            for (int m = 0; m < VT; ++m) {
+              o[m] *= 1.0f / unit;
+              o[m] = add_product(is_low, value_operand(vs, h, m), p, o[m]);
+              o[m] *= unit;
+              __builtin_amdgcn_sched_barrier(0);
+            }
+          }
         } else {
           // Slots behind the last entry hold what was there before: taken as 0.
           const int valid = used - slot0;
           auto both = [&](int t) { return (t < valid ? 0xFFFFu : 0u) | (t + 1 < valid ? 0xFFFF0000u : 0u); };
-          const uint32_t vs = fresh(unit_at(i) + v_at);
           auto operand = [&](int h, int m) {
             const uint4 x = value_operand(vs, h, m);
             const int t = 16 * h + 4 * g;
@@ -559,8 +542,9 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a, int
           for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int m = 0; m < VT; ++m) wild |= abs_max_bits8(operand(h, m)) >= 0x7F80u;
+          __builtin_amdgcn_sched_barrier(0);
           if (__ballot(wild)) {
-            add_seen_values<VT, kTile>(s_kv[(i >> 1) % 3] + (i & 1) * 2 * kTile + kValues, s, hidden, o, g, n);
+            add_seen_values<VT, kTile>(s_kv[slot] + (i & 1) * 2 * kTile + kValues, s, hidden, o, g, n);
           } else {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -571,7 +555,9 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a, int
           }
         }
       }
-      meet(i);
+      if (!(i & 1)) meet(is_low, i >> 1);
+      else slot = after(slot);
+      ++i;
     }
   };
   const int u_low = 2 * low_steps, u_high = 2 * (low_steps + high_steps), u_end = 2 * j_end;
