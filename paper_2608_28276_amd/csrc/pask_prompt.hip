@@ -85,21 +85,15 @@ __device__ __forceinline__ int entries_at(const int32_t* list, int n, int n_pos,
   return entries_below(list, max(0, n - (n_pos - x)), min(n, x), x);
 }
 
-// Code j of a word times its scale s, exact in fp32 (a code has 3 bits, a scale 11).  Codes in byte order: the low
-// nibbles of bytes 0..3, then the high ones (LOW keys: 8 elements of a chunk; LOW values: 4 slots of one dimension,
-// then of the one 16 on).
-__device__ __forceinline__ float code_value(uint32_t w, int j, float s) {
-  const uint32_t n = j < 4 ? (w >> (8 * j)) & 15u : (w >> (8 * (j - 4) + 4)) & 15u;
-  return fmaf((float)n, s, -8.0f * s);
-}
-// The high halves of two fp32 as a pair of bf16 (their upper 8 significant bits), and what is left of them, at most 6
-// bits, as another: together the two fp32, where they have 14 bits.
-__device__ __forceinline__ uint32_t split_pair(float x, float y, uint32_t& rest) {
-  const uint32_t a = __float_as_uint(x), b = __float_as_uint(y);
-  const uint32_t r = __float_as_uint(x - __uint_as_float(a & 0xFFFF0000u));
-  const uint32_t q = __float_as_uint(y - __uint_as_float(b & 0xFFFF0000u));
-  rest = __builtin_amdgcn_perm(q, r, 0x07060302u);
-  return __builtin_amdgcn_perm(b, a, 0x07060302u);
+// Pairs of fp16 in a word.
+__device__ __forceinline__ f16x2_t halves(uint32_t w) { return __builtin_bit_cast(f16x2_t, w); }
+__device__ __forceinline__ uint32_t word_of(f16x2_t h) { return __builtin_bit_cast(uint32_t, h); }
+// Codes of a word as fp16 (1024 + n has its last bit at 1): pair x holds the nibbles x = 0: 0 and 4, 1: 2 and 6,
+// 2: 1 and 5, 3: 3 and 7, that is the elements 0 and 2, 1 and 3, 4 and 6, 5 and 7 of a key's eight, or slots 0 and 2, 1
+// and 3 of a value's dimension, then of the one 16 on.
+__device__ __forceinline__ f16x2_t code_pair(uint32_t w, int x) {
+  const uint32_t n = (w >> (x == 0 ? 0 : x == 1 ? 8 : x == 2 ? 4 : 12)) & 0x000F000Fu;
+  return halves(n | 0x64006400u) - halves(0x64086408u);
 }
 
 // Codes and scales of one thread's share of a LOW page: quarter q of slot t's
@@ -111,8 +105,10 @@ struct LowPart {
   uint32_t code[NG];
   uint32_t scale[2 * NG];                          // keys: the first NG / 2
 };
-// A page with a scale above this holds values that fp16 does not; it is taken at 1 / 16 of them.
-constexpr float kWideScale = 65504.0f / 7.0f, kWide = 16.0f;
+// A page with a scale above this (fp16 bits of 65504 / 7, rounded down) holds elements that fp16 does not; it is taken
+// at 1 / 16 of them.
+constexpr uint32_t kWideScale = 0x7091u;
+constexpr float kWide = 16.0f;
 
 // O += P V key by key over 32 keys (values of 2 pages at s_v), where a value
 // that some query does not see is infinite or NaN (a weight of 0 times it is
@@ -161,12 +157,14 @@ __device__ __forceinline__ void add_seen_values(const uint8_t* s_v, f32x16_t s, 
 // the scores' lane layout is the operand layout of P up to the order of the 16
 // slots of a page, which two halves 512 bytes apart follow).  So HIGH pages go
 // to LDS as they lie, and every operand read is contiguous.
-// LOW pages are widened on the way, once for all rows of the workgroup: a key,
-// code times scale with up to 14 bits, as the sum of two bf16 (exact; its
-// scores take twice the products, half as many again in all), a value rounded
-// once to fp16 (half a step, 2^-11), with weights of fp16.  Keys of one bf16
-// made the outputs of int4 histories 3.4e-3 of their size wrong and lse 3e-5;
-// outputs of bf16 pages are 2.1e-3 wrong, most of it their own rounding.
+// LOW pages are widened to fp16 on the way, once for all rows of the workgroup,
+// by packed products.  A key is code * (s8 + s3), the scale's upper 8 bits and
+// its last 3: two exact fp16, whose scores take twice the products (half as many
+// again in all); a value is rounded once (half a step, 2^-11) and meets weights
+// of fp16.  The queries become fp16 too, each row at the power of two that takes
+// its largest element below 2^15 (exact for elements down to 2^-22 of it).  Keys
+// of one bf16 made the outputs of int4 histories 3.4e-3 of their size wrong and
+// lse 3e-5; outputs of bf16 pages are 2.1e-3 wrong, most of it their own rounding.
 // The scores of the next 32 keys are computed beside the weights of the current
 // ones; two steps are on their way into a ring of three LDS buffers meanwhile.
 // The keys that a row sees are, in each store, those up to a place of its list;
@@ -178,7 +176,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a, int
   // A page in LDS: keys, the rest of LOW keys, values.
   constexpr int kPart = L::kHiV, kValues = 2 * kPart, kTile = 3 * kPart, kStep = kStepPages * kTile;
   __shared__ __align__(1024) uint8_t s_kv[3][kStep];
-  __shared__ uint32_t s_wide[3][kStepPages];       // LOW pages whose values are at 1 / 16
+  __shared__ __align__(16) uint32_t s_wide[3][2 * kStepPages];   // LOW parts (keys, values of a page) at 1 / 16
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int g = lane >> 5, n = lane & 31;
   // Workgroups go to the 8 XCDs in turn: neighbours are different KV heads.  The longest tiles first.
@@ -215,15 +213,32 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a, int
 
   // Scores are scaled by |scale|; its sign goes to the queries, so that a score's maximum is a scaled one's.
   uint4 qf[KI];
-  const uint32_t flip = a.scale_log2 < 0.0f ? 0x80008000u : 0u;
-  const float scale = fabsf(a.scale_log2);
+  float scale = 0.0f;                              // of the lane's row, as its queries are held
   const size_t q_row = (((size_t)b * a.max_q + (in ? row / G : 0)) * a.n_q_heads + (size_t)head * G + (in ? row % G : 0));
-  const uint16_t* qrow = a.q + q_row * D + 8 * g;
+  auto load_queries = [&](auto is_low) __attribute__((always_inline)) {
+    const uint32_t flip = a.scale_log2 < 0.0f ? 0x80008000u : 0u;
+    const uint16_t* qrow = a.q + q_row * D + 8 * g;
+    uint32_t most = 0u;
 #pragma unroll
-  for (int i = 0; i < KI; ++i) {
-    qf[i] = in ? *reinterpret_cast<const uint4*>(qrow + 16 * i) : make_uint4(0u, 0u, 0u, 0u);
-    qf[i] = make_uint4(qf[i].x ^ flip, qf[i].y ^ flip, qf[i].z ^ flip, qf[i].w ^ flip);
-  }
+    for (int i = 0; i < KI; ++i) {
+      qf[i] = in ? *reinterpret_cast<const uint4*>(qrow + 16 * i) : make_uint4(0u, 0u, 0u, 0u);
+      if (decltype(is_low)::value) most = max(most, abs_max_bits8(qf[i]));
+      qf[i] = make_uint4(qf[i].x ^ flip, qf[i].y ^ flip, qf[i].z ^ flip, qf[i].w ^ flip);
+    }
+    scale = fabsf(a.scale_log2);
+    if constexpr (decltype(is_low)::value) {
+      most = max(most, (uint32_t)__shfl_xor((int)most, 32));
+      const int up = 14 - ((int)(most >> 7) - 127);  // the largest goes to 2^14 ..
+      auto two = [&](float x, float y) { return pack_half2(ldexpf(x, up), ldexpf(y, up)); };
+#pragma unroll
+      for (int i = 0; i < KI; ++i) {               // in the order of code_pair
+        const uint4 q = qf[i];
+        qf[i] = make_uint4(two(bf16_lo(q.x), bf16_lo(q.y)), two(bf16_hi(q.x), bf16_hi(q.y)),
+                           two(bf16_lo(q.z), bf16_lo(q.w)), two(bf16_hi(q.z), bf16_hi(q.w)));
+      }
+      scale = ldexpf(scale, -up);
+    }
+  };
 
   // Where the head's part of a page starts in its pool, 64 pages of a kind at a time, one per lane.
   uint32_t from_lo = 0, from_hi = 0;
@@ -289,42 +304,48 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a, int
 #pragma unroll
     for (int k = 0; k < kParts; ++k) {
       const int x = wave + k * W, p = x >> 1;
+      const bool values = (x & 1) != 0;
       const int slots = keys.n[kLowPages] - (page0_of(j, kLowPages) + p) * kPage;   // of the page in use
-      auto scale_of = [&](int t, int c) {          // slot t's, half c of the scales
-        const float s = half_value((uint16_t)(low[k].scale[c >> 1] >> (16 * (c & 1))));
-        return t < slots ? s : 0.0f;
-      };
-      if (x & 1) {
-        const uint32_t at = dst + p * kTile + kValues + lane * 16;
-        const int t0 = (lane >> 4) * 4;
-        bool wide = false;
+      uint32_t (&sc)[2 * NG] = low[k].scale;
+      if (slots < kPage) {
 #pragma unroll
-        for (int c = 0; c < 4 * NG; ++c) wide |= scale_of(t0 + c / NG, c) > kWideScale;
-        const float unit = __ballot(wide) ? 1.0f / kWide : 1.0f;
+        for (int c = 0; c < 2 * NG; ++c)
+          if ((values ? (lane >> 4) * 4 + c / (NG / 2) : lane & 15) >= slots) sc[c] = 0u;
+      }
+      typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
+      u16x2_t most = __builtin_bit_cast(u16x2_t, sc[0]);
 #pragma unroll
-        for (int i = 0; i < NG; ++i) {
-          float v[8];
+      for (int c = 1; c < 2 * NG; ++c)
+        if (c < NG / 2 || values) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2_t, sc[c]));
+      const bool wide = __ballot(max(most[0], most[1]) > kWideScale) != 0ull;
+      if (wide) {
 #pragma unroll
-          for (int t = 0; t < 8; ++t) v[t] = code_value(low[k].code[i], t, scale_of(t0 + t % 4, t % 4 * NG + i) * unit);
-          write_lds16(at + i * 1024, make_uint4(pack_half2(v[0], v[1]), pack_half2(v[2], v[3]), pack_half2(v[4], v[5]),
-                                                pack_half2(v[6], v[7])));
-        }
-        if (lane == 0) s_wide[j % 3][p] = unit != 1.0f;
-      } else {
-        const uint32_t at = dst + p * kTile + lane * 16;
+        for (int c = 0; c < 2 * NG; ++c) sc[c] = word_of(halves(sc[c]) * (f16x2_t){(_Float16)(1.0f / kWide), (_Float16)(1.0f / kWide)});
+      }
+      if (lane == 0) s_wide[j % 3][x] = wide;
+      const uint32_t at = dst + p * kTile + (values ? kValues : 0) + lane * 16;
+      if (values) {
 #pragma unroll
-        for (int i = 0; i < NG; ++i) {
-          const float s = scale_of(lane & 15, i);
-          uint4 hi, lo;
-          auto two = [&](int j, uint32_t& rest) {
-            return split_pair(code_value(low[k].code[i], j, s), code_value(low[k].code[i], j + 1, s), rest);
+        for (int i = 0; i < NG; ++i) {             // half i of slot t's NG: of words (NG / 2) t + i / 2
+          const uint32_t pick = i & 1 ? 0x07060302u : 0x05040100u;
+          auto scales = [&](int t) {               // of slots t and t + 2
+            return halves(__builtin_amdgcn_perm(sc[(t + 2) * (NG / 2) + i / 2], sc[t * (NG / 2) + i / 2], pick));
           };
-          hi.x = two(0, lo.x);
-          hi.y = two(2, lo.y);
-          hi.z = two(4, lo.z);
-          hi.w = two(6, lo.w);
-          write_lds16(at + i * 1024, hi);
-          write_lds16(at + kPart + i * 1024, lo);
+          const uint32_t w = low[k].code[i];
+          write_lds16(at + i * 1024, make_uint4(word_of(code_pair(w, 0) * scales(0)), word_of(code_pair(w, 1) * scales(1)),
+                                                word_of(code_pair(w, 2) * scales(0)), word_of(code_pair(w, 3) * scales(1))));
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < NG; ++i) {
+          const uint32_t pick = i & 1 ? 0x03020302u : 0x01000100u;
+          const uint32_t both = __builtin_amdgcn_perm(sc[i / 2], sc[i / 2], pick), upper = both & 0xFFF8FFF8u;
+          const f16x2_t s8 = halves(upper), s3 = halves(both) - s8;
+          const uint32_t w = low[k].code[i];
+          const f16x2_t c[4] = {code_pair(w, 0), code_pair(w, 1), code_pair(w, 2), code_pair(w, 3)};
+          write_lds16(at + i * 1024, make_uint4(word_of(c[0] * s8), word_of(c[1] * s8), word_of(c[2] * s8), word_of(c[3] * s8)));
+          write_lds16(at + kPart + i * 1024,
+                      make_uint4(word_of(c[0] * s3), word_of(c[1] * s3), word_of(c[2] * s3), word_of(c[3] * s3)));
         }
       }
     }
@@ -353,6 +374,9 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a, int
     return read_lds16(decltype(is_low)::value ? ks + 512 * (k >> 1) + (k & 1) * kPart : ks + 512 * k);
   };
   auto query_operand = [&](auto is_low, int k) { return qf[decltype(is_low)::value ? k >> 1 : k]; };
+  auto add_product = [&](auto is_low, uint4 v, uint4 p, f32x16_t c) {
+    return decltype(is_low)::value ? mfma_half(v, p, c) : mfma(v, p, c);
+  };
   auto scores = [&](auto is_low, int i) __attribute__((always_inline)) {
     constexpr int kProducts = decltype(is_low)::value ? 2 * KI : KI;
     f32x16_t s;
@@ -364,7 +388,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a, int
     for (int k = 0; k < kAhead; ++k) ring[k] = key_operand(is_low, ks, k);
 #pragma unroll
     for (int k = 0; k < kProducts; ++k) {
-      s = mfma(ring[k % kAhead], query_operand(is_low, k), s);
+      s = add_product(is_low, ring[k % kAhead], query_operand(is_low, k), s);
       if (k + kAhead < kProducts) ring[k % kAhead] = key_operand(is_low, ks, k + kAhead);
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -387,17 +411,16 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a, int
     mx = ref;
   };
   auto packed = [](auto is_low, const f32x16_t& s, int h) {   // weights of a page's 16 slots as an operand
-    auto two = [&](int r) {
-      return decltype(is_low)::value ? pack_half2(s[8 * h + r], s[8 * h + r + 1]) : pack_bf16x2(s[8 * h + r], s[8 * h + r + 1]);
-    };
-    return make_uint4(two(0), two(2), two(4), two(6));
+    const int r = 8 * h;
+    if constexpr (decltype(is_low)::value)         // in the order of code_pair
+      return make_uint4(pack_half2(s[r], s[r + 2]), pack_half2(s[r + 1], s[r + 3]), pack_half2(s[r + 4], s[r + 6]),
+                        pack_half2(s[r + 5], s[r + 7]));
+    return make_uint4(pack_bf16x2(s[r], s[r + 1]), pack_bf16x2(s[r + 2], s[r + 3]), pack_bf16x2(s[r + 4], s[r + 5]),
+                      pack_bf16x2(s[r + 6], s[r + 7]));
   };
-  auto add_product = [&](auto is_low, uint4 v, uint4 p, f32x16_t c) {
-    return decltype(is_low)::value ? mfma_half(v, p, c) : mfma(v, p, c);
-  };
-  // Pages of a step at 1 / 16 of their values.
   auto any_wide = [&](int s) {
-    return __builtin_amdgcn_readfirstlane((int)(s_wide[s][0] | s_wide[s][1] | s_wide[s][2] | s_wide[s][3])) != 0;
+    const uint4 x = *reinterpret_cast<const uint4*>(s_wide[s]), y = *reinterpret_cast<const uint4*>(s_wide[s] + 4);
+    return __builtin_amdgcn_readfirstlane((int)(x.x | x.y | x.z | x.w | y.x | y.y | y.z | y.w)) != 0;
   };
 
   // Units of 32 keys.  After a step's first unit the workgroup meets: the next
@@ -436,7 +459,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a, int
     for (int x = 0; x < kAll; ++x) {
       if (x >= kProducts && (x - kProducts) % VT == 0) p = packed(is_low, s, (x - kProducts) / VT);
       if (x < kProducts) {
-        next = mfma(ring[x % kAhead], query_operand(is_low, x), next);
+        next = add_product(is_low, ring[x % kAhead], query_operand(is_low, x), next);
       } else {
         const int m = (x - kProducts) % VT;
         o[m] = add_product(is_low, ring[x % kAhead], p, o[m]);
@@ -504,6 +527,12 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a, int
           hidden |= (uint32_t)hid << r;
         }
         s = scores(is_low, i);
+        if constexpr (decltype(is_low)::value)
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+            if (s_wide[slot][4 * (i & 1) + 2 * h])
+#pragma unroll
+              for (int r = 0; r < 8; ++r) s[8 * h + r] *= kWide;
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] = hidden >> r & 1u ? -INFINITY : s[r];
         refer(highest(s));
@@ -519,7 +548,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a, int
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             const uint4 p = packed(is_low, s, h);
-            const float unit = s_wide[slot][2 * (i & 1) + h] ? kWide : 1.0f;
+            const float unit = s_wide[slot][4 * (i & 1) + 2 * h + 1] ? kWide : 1.0f;
 #pragma unroll
             for (int m = 0; m < VT; ++m) {
               o[m] *= 1.0f / unit;
@@ -561,8 +590,11 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a, int
     }
   };
   const int u_low = 2 * low_steps, u_high = 2 * (low_steps + high_steps), u_end = 2 * j_end;
-  if (i < min(u_low, u_end))
+  if (i < min(u_low, u_end)) {
+    load_queries(std::true_type{});
     segment(std::true_type{}, false, 0, min(u_low, u_end), first_sees[0], last_sees[0], keys.list[0], keys.n[0]);
+  }
+  if (i < u_end) load_queries(std::false_type{});
 #pragma unroll 1
   for (int k = 0; k < 2; ++k) {                    // HIGH entries, then the window's
     const int to = k ? u_end : min(u_high, u_end);
