@@ -44,6 +44,14 @@ __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {   // round 
   return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t){lo, hi}, f16x2_t));
 }
 
+// 16 bytes per lane from src (the same for the wave) + at into LDS: lane l's to
+// lds + 16 l.  In asm because the compiler waits for every copy it knows of
+// before the next read of LDS, that of another buffer too; these are waited for
+// at the workgroup's meetings alone (wait_loads).  No register is written.
+__device__ __forceinline__ void copy_to_lds(const uint8_t* src, uint32_t at, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(at), "s"(src), "s"(lds) : "memory", "m0");
+}
+
 // The kinds of pages a sequence's keys come from, in the order they are taken.
 enum Kind { kLowPages = 0, kHighPages = 1, kWindowPages = 2 };
 
@@ -243,42 +251,51 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
     }
   };
 
-  // Where the head's part of a page starts in its pool, 64 pages of a kind at a time, one per lane.
-  uint32_t from_lo = 0, from_hi = 0;
-  int from_of = -1;                                // kind and block of 64 pages that are held
-  auto page_at = [&](int kind, int p) {            // p: the same for the wave
-    const int of = (p >> 6) * 4 + kind;
-    if (of != from_of) {
-      const int at = (p & ~63) + lane;             // pages behind the last one repeat it
-      const int page = kind == kWindowPages ? keys.ring_page + min(at, a.cv.ring_pp - 1)
-                       : kind == kLowPages  ? keys.table[0][min(at, (n_see[0] - 1) >> 4)]
-                                            : keys.table[1][min(at, (n_see[1] - 1) >> 4)];
-      const uint32_t hs = ((uint32_t)head + (uint32_t)page) % (uint32_t)a.cv.n_kv_heads;
-      const uint64_t from = kind == kLowPages ? (uint64_t)page * a.cv.lo_page_bytes + hs * (uint32_t)L::kLoHead
-                                              : (uint64_t)page * a.cv.hi_page_bytes + hs * (uint32_t)L::kHiHead;
-      from_lo = (uint32_t)from;
-      from_hi = (uint32_t)(from >> 32);
-      from_of = of;
-    }
-    const uint32_t lo = __builtin_amdgcn_readlane(from_lo, p & 63), hi = __builtin_amdgcn_readlane(from_hi, p & 63);
-    return (kind == kLowPages ? a.cv.lo_pool : a.cv.hi_pool) + ((uint64_t)hi << 32 | lo);
-  };
   // The kind of the tile's step j and its first page.
   auto kind_of = [&](int j) { return j < low_steps ? kLowPages : j < low_steps + high_steps ? kHighPages : kWindowPages; };
   auto page0_of = [&](int j, int kind) {
     return kStepPages * (j - (kind == kLowPages ? 0 : kind == kHighPages ? low_steps : low_steps + high_steps));
+  };
+  // Where the head's part of a step's pages starts, 16 steps at a time, one page
+  // per lane; pages behind the last one, and steps behind the last one, repeat it.
+  uint32_t from_lo = 0, from_hi = 0;
+  int from_of = -1;                                // which 16 steps
+  auto look_up = [&](int j) __attribute__((always_inline)) {
+    if ((j >> 4) == from_of) return;
+    from_of = j >> 4;
+    const int jl = min((j & ~15) + (lane >> 2), j_end - 1), kind = kind_of(jl), p = page0_of(jl, kind) + (lane & 3);
+    const int page = kind == kWindowPages ? keys.ring_page + min(p, a.cv.ring_pp - 1)
+                     : kind == kLowPages  ? keys.table[0][min(p, (n_see[0] - 1) >> 4)]
+                                          : keys.table[1][min(p, (n_see[1] - 1) >> 4)];
+    const uint32_t hs = ((uint32_t)head + (uint32_t)page) % (uint32_t)a.cv.n_kv_heads;
+    const uint64_t at = kind == kLowPages ? (uint64_t)a.cv.lo_pool + (uint64_t)page * a.cv.lo_page_bytes + hs * (uint32_t)L::kLoHead
+                                          : (uint64_t)a.cv.hi_pool + (uint64_t)page * a.cv.hi_page_bytes + hs * (uint32_t)L::kHiHead;
+    from_lo = (uint32_t)at;
+    from_hi = (uint32_t)(at >> 32);
+  };
+  auto page_at = [&](int j, int k) {               // page k of step j, looked up
+    const int l = (j & 15) * kStepPages + k;
+    return reinterpret_cast<const uint8_t*>((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)from_hi, l) << 32 |
+                                            (uint32_t)__builtin_amdgcn_readlane((int)from_lo, l));
+  };
+  // Copies of a HIGH or window step into LDS: instruction x of kCopies of this wave.
+  constexpr int kInstr = L::kHiHead / 1024, kCopies = (kStepPages * kInstr + W - 1) / W;   // 1 KiB each; of a page
+  auto copy = [&](int j, int k) __attribute__((always_inline)) {
+    const int x = wave + k * W, y = x % kInstr;
+    copy_to_lds(page_at(j, x / kInstr), (uint32_t)(y * 1024 + lane * 16),
+                lds_address(s_kv[0]) + j % 3 * kStep + (x / kInstr) * kTile + y * 1024 + (y < kInstr / 2 ? 0 : kValues - kPart));
   };
   // A LOW step's parts of this wave: part x is the keys (x even) or values of page x / 2.
   constexpr int kParts = (2 * kStepPages + W - 1) / W;
   LowPart<D> low[kParts];
   auto fetch = [&](auto low_too, int j) __attribute__((always_inline)) {
     if (j >= j_end) return;
-    const int kind = kind_of(j), p0 = page0_of(j, kind);
-    if (decltype(low_too)::value && kind == kLowPages) {
+    look_up(j);
+    if (decltype(low_too)::value && kind_of(j) == kLowPages) {
 #pragma unroll
       for (int k = 0; k < kParts; ++k) {
         const int x = wave + k * W;
-        const uint8_t* src = page_at(kind, p0 + (x >> 1));
+        const uint8_t* src = page_at(j, x >> 1);
         const bool values = (x & 1) != 0;
         const uint32_t* code = reinterpret_cast<const uint32_t*>(src + (values ? L::kLoVC : 0)) + lane * NG;
         const uint32_t* scale_at = reinterpret_cast<const uint32_t*>(src + (values ? L::kLoVS : L::kLoKS));
@@ -291,14 +308,8 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
       }
       return;
     }
-    uint8_t* dst = s_kv[j % 3];
-    constexpr int kInstr = L::kHiHead / 1024;      // of a page
 #pragma unroll
-    for (int k = 0; k < (kStepPages * kInstr + W - 1) / W; ++k) {
-      const int x = wave + k * W, y = x % kInstr;
-      load_to_lds<false>(page_at(kind, p0 + x / kInstr) + y * 1024 + lane * 16,
-                         dst + (x / kInstr) * kTile + y * 1024 + (y < kInstr / 2 ? 0 : kValues - kPart));
-    }
+    for (int k = 0; k < kCopies; ++k) copy(j, k);
   };
   // A LOW step's arrived parts into its buffer, widened; slots behind the last entry as 0.
   auto land = [&](int j) __attribute__((always_inline)) {
@@ -367,9 +378,10 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
   int slot = j_begin % 3;                          // buffer of the current unit's step
   auto after = [](int s) { return s == 2 ? 0 : s + 1; };
   auto unit_at = [&](int s, int i) { return lds_address(s_kv[0]) + s * kStep + (i & 1) * 2 * kTile; };
-  auto value_operand = [&](uint32_t vs, int h, int m) {
-    const uint32_t at = vs + h * kTile + m * 1024;
-    const u32x2_t x = *(const lds_u32x2*)(uintptr_t)at, y = *(const lds_u32x2*)(uintptr_t)(at + 512);
+  // Two reads of 8 bytes, as 4.1 cycles, where one instruction of both (ds_read2st64_b64) takes 8.1.
+  auto value_operand = [&](uint32_t vs, uint32_t vs2, int h, int m) {
+    const u32x2_t x = *(const lds_u32x2*)(uintptr_t)(vs + h * kTile + m * 1024);
+    const u32x2_t y = *(const lds_u32x2*)(uintptr_t)(vs2 + h * kTile + m * 1024);
     return make_uint4(x[0], x[1], y[0], y[1]);
   };
   // Operand k of a unit's scores: with LOW keys each part of the queries meets both of the key.
@@ -397,15 +409,15 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
     }
     return s;
   };
-  auto highest = [&](const f32x16_t& s) {          // of the lane's row, scaled
+  auto highest = [&](const f32x16_t& s) {          // of the lane's part of its row, scaled
     float top = fmaxf(s[0], s[1]);
 #pragma unroll
     for (int r = 2; r < 16; ++r) top = fmaxf(top, s[r]);
-    top = fmaxf(top, __shfl_xor(top, 32));
     return top == -INFINITY ? top : top * scale;
   };
   auto exceeds = [&](float top) { return __ballot(top > mx + kHeadroom) != 0ull; };
   auto refer = [&](float top) __attribute__((always_inline)) {   // the reference follows a maximum that exceeds it
+    top = fmaxf(top, __shfl_xor(top, 32));
     const float ref = top > mx + kHeadroom ? top - kBelow : mx;
     const float alpha = ref == mx ? 1.0f : __builtin_amdgcn_exp2f(mx - ref);
     sum *= alpha;
@@ -433,7 +445,6 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
     wait_loads();
     if (decltype(is_low)::value) land(j + 1);      // LOW steps come first
     __syncthreads();
-    fetch(is_low, j + 2);
   };
   if (j_begin < j_end) {
     fetch(std::true_type{}, j_begin);
@@ -444,13 +455,13 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
   }
   // Unit i's scores s become weights and add its values, beside the scores of unit i + 1.
   float base = 0.0f, odd_sum = 0.0f, top = -INFINITY;
-  auto turn = [&](auto is_low, auto is_odd, int i, f32x16_t& s, f32x16_t& next) __attribute__((always_inline)) {
+  auto turn = [&](auto is_low, auto is_odd, int j_next, f32x16_t& s, f32x16_t& next) __attribute__((always_inline)) {
     constexpr int kProducts = decltype(is_low)::value ? 2 * KI : KI, kAll = kProducts + 2 * VT;
     constexpr bool kOdd = decltype(is_odd)::value;
     const uint32_t ks = fresh(unit_at(kOdd ? after(slot) : slot, kOdd ? 0 : 1) + k_at);
-    const uint32_t vs = fresh(unit_at(slot, kOdd ? 1 : 0) + v_at);
+    const uint32_t vs = fresh(unit_at(slot, kOdd ? 1 : 0) + v_at), vs2 = fresh(vs + 512);
     auto operand = [&](int x) {
-      return x < kProducts ? key_operand(is_low, ks, x) : value_operand(vs, (x - kProducts) / VT, (x - kProducts) % VT);
+      return x < kProducts ? key_operand(is_low, ks, x) : value_operand(vs, vs2, (x - kProducts) / VT, (x - kProducts) % VT);
     };
 #pragma unroll
     for (int r = 0; r < 16; ++r) next[r] = 0.0f;
@@ -468,14 +479,17 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
         o[m] = add_product(is_low, ring[x % kAhead], p, o[m]);
       }
       if (x + kAhead < kAll) ring[x % kAhead] = operand(x + kAhead);
-      if (x < kProducts)
 #pragma unroll
-        for (int r = 16 * x / kProducts; r < 16 * (x + 1) / kProducts; ++r) {
+      for (int r = 0; r < 16; ++r)
+        if (r * (kProducts + VT - 1) / 16 == x) {  // the first 8 before the first values, all before the second's
           s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale, -base));
           if (r & 1) odd_sum += s[r];
           else sum += s[r];
         }
-      if (x == kProducts) top = highest(next);
+      if (x == kProducts + VT) top = highest(next);
+      // The step after next, in the odd unit, its copies between the products: issued together behind the barrier they
+      // and their addresses took a fifth of the call.
+      if (kOdd && !decltype(is_low)::value && x % 3 == 1 && x / 3 < kCopies) copy(j_next, x / 3);
       __builtin_amdgcn_sched_barrier(0);
     }
   };
@@ -499,22 +513,34 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
     const int whole = min(u1, u0 + fs / 32);       // the units that all rows of the wave see whole
     while (i < u1) {
       f32x16_t s;
-      // Steps whose units are whole.  The loop is left to move the reference and at wide pages.
+      // Steps whose units are whole, up to a wide page.
       if (!(i & 1) && i + 1 < whole && !(decltype(is_low)::value && any_wide(slot))) {
         f32x16_t t;
         s = scores(is_low, i);
         refer(highest(s));
         base = mx;
-        for (;;) {
-          turn(is_low, std::false_type{}, i, s, t);
+        auto follow = [&] {                        // rarely: the reference behind the next scores' maximum
+          if (!exceeds(top)) return;
+          sum += odd_sum;
+          odd_sum = 0.0f;
+          refer(top);
+          base = mx;
+        };
+        bool more;
+        do {                                       // (one way out: a second one costs copies of the sums)
+          const int j_next = (i >> 1) + 2;
+          turn(is_low, std::false_type{}, j_next, s, t);
           meet(is_low, i >> 1);
-          ++i;
-          if (exceeds(top)) break;
-          turn(is_low, std::true_type{}, i, t, s);
-          ++i;
+          follow();
+          if (decltype(is_low)::value) fetch(is_low, j_next);
+          else look_up(j_next);
+          turn(is_low, std::true_type{}, j_next, t, s);
+          i += 2;
           slot = after(slot);
-          if (exceeds(top) || i + 1 >= whole || (decltype(is_low)::value && any_wide(slot))) break;
-        }
+          more = i + 1 < whole && !(decltype(is_low)::value && any_wide(slot));
+          if (!more) top = -INFINITY;              // the scores in s are of no use
+          follow();
+        } while (more);
         sum += odd_sum;
         odd_sum = 0.0f;
         if (i >= u1) break;
@@ -546,7 +572,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
           s[r] = hidden >> r & 1u ? 0.0f : w;
           sum += s[r];
         }
-        const uint32_t vs = fresh(unit_at(slot, i) + v_at);
+        const uint32_t vs = fresh(unit_at(slot, i) + v_at), vs2 = fresh(vs + 512);
         if constexpr (decltype(is_low)::value) {
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
@@ -555,7 +581,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
 #pragma unroll
             for (int m = 0; m < VT; ++m) {
               o[m] *= 1.0f / unit;
-              o[m] = add_product(is_low, value_operand(vs, h, m), p, o[m]);
+              o[m] = add_product(is_low, value_operand(vs, vs2, h, m), p, o[m]);
               o[m] *= unit;
               __builtin_amdgcn_sched_barrier(0);
             }
@@ -565,7 +591,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
           const int valid = used - slot0;
           auto both = [&](int t) { return (t < valid ? 0xFFFFu : 0u) | (t + 1 < valid ? 0xFFFF0000u : 0u); };
           auto operand = [&](int h, int m) {
-            const uint4 x = value_operand(vs, h, m);
+            const uint4 x = value_operand(vs, vs2, h, m);
             const int t = 16 * h + 4 * g;
             return make_uint4(x.x & both(t), x.y & both(t + 2), x.z & both(t + 8), x.w & both(t + 10));
           };
@@ -587,8 +613,12 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
           }
         }
       }
-      if (!(i & 1)) meet(is_low, i >> 1);
-      else slot = after(slot);
+      if (!(i & 1)) {
+        meet(is_low, i >> 1);
+        fetch(is_low, (i >> 1) + 2);
+      } else {
+        slot = after(slot);
+      }
       ++i;
     }
   };
@@ -605,6 +635,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
     segment(std::false_type{}, k == 1, k ? u_high : u_low, to, k ? 0 : first_sees[1], k ? 0 : last_sees[1], keys.list[1],
             k ? keys.ring_slots : keys.n[1]);
   }
+  wait_loads();                                    // copies that repeat the last step: none is left behind
   sum += __shfl_xor(sum, 32);
   if (!in) return;
   if (a.pieces > 1) {
