@@ -48,8 +48,15 @@ __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {   // round 
 // lds + 16 l.  In asm because the compiler waits for every copy it knows of
 // before the next read of LDS, that of another buffer too; these are waited for
 // at the workgroup's meetings alone (wait_loads).  No register is written.
+// kOnce: data read once per call (non-temporal).
+template <bool kOnce>
 __device__ __forceinline__ void copy_to_lds(const uint8_t* src, uint32_t at, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(at), "s"(src), "s"(lds) : "memory", "m0");
+  if constexpr (kOnce)
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(at), "s"(src), "s"(lds)
+                 : "memory", "m0");
+  else
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(at), "s"(src), "s"(lds)
+                 : "memory", "m0");
 }
 
 // The kinds of pages a sequence's keys come from, in the order they are taken.
@@ -118,14 +125,14 @@ struct LowPart {
 constexpr uint32_t kWideScale = 0x7091u;
 constexpr float kWide = 16.0f;
 
-// O += P V key by key over 32 keys (values of 2 pages at s_v), where a value
+// O += P V key by key over 32 keys (values of pages at v0 and v1), where a value
 // that some query does not see is infinite or NaN (a weight of 0 times it is
 // not 0): only what a query sees is added.  Lane (g, n) holds the weights of
 // query n for half of the keys, and which of them are hidden; lane (1 - g, n)
 // the others'.
-template <int VT, int kTile>
-__device__ __forceinline__ void add_seen_values(const uint8_t* s_v, f32x16_t s, uint32_t hidden, f32x16_t (&o)[VT], int g,
-                                                int n) {
+template <int VT>
+__device__ __forceinline__ void add_seen_values(const uint8_t* v0, const uint8_t* v1, f32x16_t s, uint32_t hidden,
+                                                f32x16_t (&o)[VT], int g, int n) {
 #pragma unroll 1
   for (int x = 0; x < 16; ++x) {
     asm volatile("" : "+v"(g));                    // no code: keeps this rare path's addresses out of the loops around it
@@ -143,12 +150,87 @@ __device__ __forceinline__ void add_seen_values(const uint8_t* s_v, f32x16_t s, 
 #pragma unroll
         for (int r = 0; r < 16; ++r) {             // element 32 m + d
           const int d = 8 * (r >> 2) + 4 * g + (r & 3);
-          const uint8_t* at = s_v + (t >> 4) * kTile + m * 1024 + ((t & 15) >> 2) * 256 + (d & 15) * 16 + (d >> 4) * 8 +
-                              (t & 3) * 2;
+          const uint8_t* at = (t & 16 ? v1 : v0) + m * 1024 + ((t & 15) >> 2) * 256 + (d & 15) * 16 + (d >> 4) * 8 + (t & 3) * 2;
           o[m][r] += p * bf16_lo(*reinterpret_cast<const uint16_t*>(at));
         }
     }
   }
+}
+
+// A row's queries as operands: lane (g, n) holds the chunks 2 i + g of row n.
+// Scores are scaled by |scale|; its sign goes to the queries, so that a score's
+// maximum is a scaled one's.  For LOW keys they are fp16, in code_pair's order,
+// the row's largest at 2^14 .. and `scale` taken along.
+template <bool kLow, int KI>
+__device__ __forceinline__ void load_queries(const PromptArgs& a, size_t q_row, bool in, int g, uint4 (&qf)[KI], float& scale) {
+  const uint32_t flip = a.scale_log2 < 0.0f ? 0x80008000u : 0u;
+  const uint16_t* qrow = a.q + q_row * (16 * KI) + 8 * g;
+  uint32_t most = 0u;
+#pragma unroll
+  for (int i = 0; i < KI; ++i) {
+    qf[i] = in ? *reinterpret_cast<const uint4*>(qrow + 16 * i) : make_uint4(0u, 0u, 0u, 0u);
+    if (kLow) most = max(most, abs_max_bits8(qf[i]));
+    qf[i] = make_uint4(qf[i].x ^ flip, qf[i].y ^ flip, qf[i].z ^ flip, qf[i].w ^ flip);
+  }
+  scale = fabsf(a.scale_log2);
+  if constexpr (kLow) {
+    most = max(most, (uint32_t)__shfl_xor((int)most, 32));
+    const int up = 14 - ((int)(most >> 7) - 127);
+    auto two = [&](float x, float y) { return pack_half2(ldexpf(x, up), ldexpf(y, up)); };
+#pragma unroll
+    for (int i = 0; i < KI; ++i) {
+      const uint4 q = qf[i];
+      qf[i] = make_uint4(two(bf16_lo(q.x), bf16_lo(q.y)), two(bf16_hi(q.x), bf16_hi(q.y)),
+                         two(bf16_lo(q.z), bf16_lo(q.w)), two(bf16_hi(q.z), bf16_hi(q.w)));
+    }
+    scale = ldexpf(scale, -up);
+  }
+}
+// Weights of a page's 16 slots as an operand; for LOW values in code_pair's order.
+template <bool kLow>
+__device__ __forceinline__ uint4 packed_weights(const f32x16_t& s, int h) {
+  const int r = 8 * h;
+  if constexpr (kLow)
+    return make_uint4(pack_half2(s[r], s[r + 2]), pack_half2(s[r + 1], s[r + 3]), pack_half2(s[r + 4], s[r + 6]),
+                      pack_half2(s[r + 5], s[r + 7]));
+  return make_uint4(pack_bf16x2(s[r], s[r + 1]), pack_bf16x2(s[r + 2], s[r + 3]), pack_bf16x2(s[r + 4], s[r + 5]),
+                    pack_bf16x2(s[r + 6], s[r + 7]));
+}
+typedef __attribute__((address_space(3))) uint32_t lds_u32;
+__device__ __forceinline__ uint32_t read_lds4(uint32_t lds) { return *(const lds_u32*)(uintptr_t)lds; }
+// N words of LDS, aligned to all of them up to 16 bytes.
+template <int N>
+__device__ __forceinline__ void read_words(uint32_t lds, uint32_t (&x)[N]) {
+  if constexpr (N == 1) {
+    x[0] = read_lds4(lds);
+  } else if constexpr (N == 2) {
+    const u32x2_t v = *(const lds_u32x2*)(uintptr_t)lds;
+    x[0] = v[0];
+    x[1] = v[1];
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+      const uint4 v = read_lds16(lds + 4 * i);
+      x[i] = v.x;
+      x[i + 1] = v.y;
+      x[i + 2] = v.z;
+      x[i + 3] = v.w;
+    }
+  }
+}
+// Copies into LDS: all but the last N that the wave issued have arrived.
+template <int N>
+__device__ __forceinline__ void wait_copies() {
+  static_assert(N < 64, "vmcnt has 6 bits");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | (N >> 4) << 14);
+  asm volatile("" ::: "memory");
+}
+// The wave's reads of LDS so far are done.
+__device__ __forceinline__ void lds_barrier_wave() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xC07F);              // lgkmcnt(0)
+  asm volatile("" ::: "memory");
 }
 
 // A workgroup of W waves takes 32 W rows of one KV head, row x being head x % G
@@ -222,34 +304,9 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
   const int steps = low_steps + high_steps + ring_steps;
   const int j_begin = (int)((long long)steps * piece / a.pieces), j_end = (int)((long long)steps * (piece + 1) / a.pieces);
 
-  // Scores are scaled by |scale|; its sign goes to the queries, so that a score's maximum is a scaled one's.
   uint4 qf[KI];
   float scale = 0.0f;                              // of the lane's row, as its queries are held
   const size_t q_row = (((size_t)b * a.max_q + (in ? row / G : 0)) * a.n_q_heads + (size_t)head * G + (in ? row % G : 0));
-  auto load_queries = [&](auto is_low) __attribute__((always_inline)) {
-    const uint32_t flip = a.scale_log2 < 0.0f ? 0x80008000u : 0u;
-    const uint16_t* qrow = a.q + q_row * D + 8 * g;
-    uint32_t most = 0u;
-#pragma unroll
-    for (int i = 0; i < KI; ++i) {
-      qf[i] = in ? *reinterpret_cast<const uint4*>(qrow + 16 * i) : make_uint4(0u, 0u, 0u, 0u);
-      if (decltype(is_low)::value) most = max(most, abs_max_bits8(qf[i]));
-      qf[i] = make_uint4(qf[i].x ^ flip, qf[i].y ^ flip, qf[i].z ^ flip, qf[i].w ^ flip);
-    }
-    scale = fabsf(a.scale_log2);
-    if constexpr (decltype(is_low)::value) {
-      most = max(most, (uint32_t)__shfl_xor((int)most, 32));
-      const int up = 14 - ((int)(most >> 7) - 127);  // the largest goes to 2^14 ..
-      auto two = [&](float x, float y) { return pack_half2(ldexpf(x, up), ldexpf(y, up)); };
-#pragma unroll
-      for (int i = 0; i < KI; ++i) {               // in the order of code_pair
-        const uint4 q = qf[i];
-        qf[i] = make_uint4(two(bf16_lo(q.x), bf16_lo(q.y)), two(bf16_hi(q.x), bf16_hi(q.y)),
-                           two(bf16_lo(q.z), bf16_lo(q.w)), two(bf16_hi(q.z), bf16_hi(q.w)));
-      }
-      scale = ldexpf(scale, -up);
-    }
-  };
 
   // The kind of the tile's step j and its first page.
   auto kind_of = [&](int j) { return j < low_steps ? kLowPages : j < low_steps + high_steps ? kHighPages : kWindowPages; };
@@ -282,7 +339,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
   constexpr int kInstr = L::kHiHead / 1024, kCopies = (kStepPages * kInstr + W - 1) / W;   // 1 KiB each; of a page
   auto copy = [&](int j, int k) __attribute__((always_inline)) {
     const int x = wave + k * W, y = x % kInstr;
-    copy_to_lds(page_at(j, x / kInstr), (uint32_t)(y * 1024 + lane * 16),
+    copy_to_lds<false>(page_at(j, x / kInstr), (uint32_t)(y * 1024 + lane * 16),
                 lds_address(s_kv[0]) + j % 3 * kStep + (x / kInstr) * kTile + y * 1024 + (y < kInstr / 2 ? 0 : kValues - kPart));
   };
   // A LOW step's parts of this wave: part x is the keys (x even) or values of page x / 2.
@@ -425,14 +482,6 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
     for (int m = 0; m < VT; ++m) o[m] *= alpha;
     mx = ref;
   };
-  auto packed = [](auto is_low, const f32x16_t& s, int h) {   // weights of a page's 16 slots as an operand
-    const int r = 8 * h;
-    if constexpr (decltype(is_low)::value)         // in the order of code_pair
-      return make_uint4(pack_half2(s[r], s[r + 2]), pack_half2(s[r + 1], s[r + 3]), pack_half2(s[r + 4], s[r + 6]),
-                        pack_half2(s[r + 5], s[r + 7]));
-    return make_uint4(pack_bf16x2(s[r], s[r + 1]), pack_bf16x2(s[r + 2], s[r + 3]), pack_bf16x2(s[r + 4], s[r + 5]),
-                      pack_bf16x2(s[r + 6], s[r + 7]));
-  };
   auto any_wide = [&](int s) {
     const uint4 x = *reinterpret_cast<const uint4*>(s_wide[s]), y = *reinterpret_cast<const uint4*>(s_wide[s] + 4);
     return __builtin_amdgcn_readfirstlane((int)(x.x | x.y | x.z | x.w | y.x | y.y | y.z | y.w)) != 0;
@@ -471,7 +520,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
     // Pinned order: a product, the read of an operand to come, a part of the weights.
 #pragma unroll
     for (int x = 0; x < kAll; ++x) {
-      if (x >= kProducts && (x - kProducts) % VT == 0) p = packed(is_low, s, (x - kProducts) / VT);
+      if (x >= kProducts && (x - kProducts) % VT == 0) p = packed_weights<decltype(is_low)::value>(s, (x - kProducts) / VT);
       if (x < kProducts) {
         next = add_product(is_low, ring[x % kAhead], query_operand(is_low, x), next);
       } else {
@@ -576,7 +625,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
         if constexpr (decltype(is_low)::value) {
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const uint4 p = packed(is_low, s, h);
+            const uint4 p = packed_weights<decltype(is_low)::value>(s, h);
             const float unit = s_wide[slot][4 * (i & 1) + 2 * h + 1] ? kWide : 1.0f;
 #pragma unroll
             for (int m = 0; m < VT; ++m) {
@@ -602,11 +651,12 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
             for (int m = 0; m < VT; ++m) wild |= abs_max_bits8(operand(h, m)) >= 0x7F80u;
           __builtin_amdgcn_sched_barrier(0);
           if (__ballot(wild)) {
-            add_seen_values<VT, kTile>(s_kv[slot] + (i & 1) * 2 * kTile + kValues, s, hidden, o, g, n);
+            const uint8_t* v0 = s_kv[slot] + (i & 1) * 2 * kTile + kValues;
+            add_seen_values<VT>(v0, v0 + kTile, s, hidden, o, g, n);
           } else {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              const uint4 p = packed(is_low, s, h);
+              const uint4 p = packed_weights<decltype(is_low)::value>(s, h);
 #pragma unroll
               for (int m = 0; m < VT; ++m) o[m] = mfma(operand(h, m), p, o[m]);
             }
@@ -624,10 +674,10 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
   };
   const int u_low = 2 * low_steps, u_high = 2 * (low_steps + high_steps), u_end = 2 * j_end;
   if (i < min(u_low, u_end)) {
-    load_queries(std::true_type{});
+    load_queries<true, KI>(a, q_row, in, g, qf, scale);
     segment(std::true_type{}, false, 0, min(u_low, u_end), first_sees[0], last_sees[0], keys.list[0], keys.n[0]);
   }
-  if (i < u_end) load_queries(std::false_type{});
+  if (i < u_end) load_queries<false, KI>(a, q_row, in, g, qf, scale);
 #pragma unroll 1
   for (int k = 0; k < 2; ++k) {                    // HIGH entries, then the window's
     const int to = k ? u_end : min(u_high, u_end);
@@ -659,32 +709,434 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
   if (a.lse && g == 0) a.lse[q_row] = sum == 0.0f ? -INFINITY : (mx + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
-// Joins the pieces of a row, one wave per row: the parts' sums and outputs,
-// taken to the largest of their references.
+// The same for few rows, where reading the pages is the work: 32 rows of one KV
+// head, the units of their keys cut over the pieces of the call and the kFewWaves
+// waves of a workgroup, which join their sums in LDS.  A wave copies pages as they
+// lie into LDS of its own and waits for no other: HIGH units in two halves, the
+// next unit's keys asked for once this one's are read, its values likewise; LOW
+// units in two batches, one taken while the other comes.  Eight waves a compute
+// unit (two workgroups) keep up to 128 KiB on its way.  LOW pages are widened in
+// registers.  Numerics are those of prompt_kernel.
+constexpr int kFewWaves = 4, kFewRows = 32, kFewMost = 64;
 template <int D, int G>
+__global__ __launch_bounds__(64 * kFewWaves, 2) void prompt_few_kernel(PromptArgs a) {
+  using L = PageLayout<D>;
+  constexpr int VT = D / 32, KI = D / 16, NG = L::NG, kPart = L::kHiV;   // kPart: bytes of a HIGH page's keys, or values
+  constexpr int kHalf = 2 * kPart / 1024;          // copies of a HIGH unit's keys, or values
+  constexpr int kLowBatch = 256 / D, kRoom = 4 * kLowBatch * L::kLoHead;   // units; bytes of a wave's LDS
+  static_assert(4 * kPart <= kRoom && kFewRows * D * 4 <= kRoom, "a wave's part of LDS");
+  __shared__ __align__(1024) uint8_t s_room[kFewWaves][kRoom];
+  __shared__ float2 s_ml[kFewWaves][kFewRows];
+  const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int g = lane >> 5, n = lane & 31;
+  int rest = (int)blockIdx.x;
+  const int head = rest % a.cv.n_kv_heads;
+  rest /= a.cv.n_kv_heads;
+  const int piece = rest % a.pieces;
+  rest /= a.pieces;
+  const int b = rest % a.batch, nq = a.n_q ? min(max(a.n_q[b], 0), a.max_q) : a.max_q, n_rows = nq * G;
+  const int row0 = rest / a.batch * kFewRows, row = row0 + n;
+  if (row0 >= n_rows) return;
+  const bool in = row < n_rows;
+  const Keys keys = keys_of(a.cv, b, a.layer);
+  const long long first = a.first ? (long long)a.first[b] : (long long)keys.n_pos - nq;
+  // Entries of each list that the first row sees, and the last.
+  const long long wave_at = first + row0 / G, wave_end = first + (min(row0 + kFewRows, n_rows) - 1) / G;
+  int first_sees[2], last_sees[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int seen = entries_at(keys.list[k], keys.n[k], keys.n_pos, lane < 32 ? wave_at : wave_end);
+    first_sees[k] = __builtin_amdgcn_readlane(seen, 0);
+    last_sees[k] = __builtin_amdgcn_readlane(seen, 32);
+  }
+  const bool ring_seen = keys.ring_slots > 0 && wave_end >= (long long)keys.n_pos - keys.ring_slots;
+  const int u_low = (last_sees[0] + 31) / 32, u_high = u_low + (last_sees[1] + 31) / 32;
+  const int units = u_high + (ring_seen ? (keys.ring_slots + 31) / 32 : 0);
+  const int part = piece * kFewWaves + wave, parts = a.pieces * kFewWaves;
+  const int begin = (int)((long long)units * part / parts), end = (int)((long long)units * (part + 1) / parts);
+  const size_t q_row = (((size_t)b * a.max_q + (in ? row / G : 0)) * a.n_q_heads + (size_t)head * G + (in ? row % G : 0));
+
+  // Where the head's part of the pages starts, 64 pages at a time, one per lane.
+  auto kind_of = [&](int u) { return u < u_low ? kLowPages : u < u_high ? kHighPages : kWindowPages; };
+  uint32_t from_lo = 0, from_hi = 0;
+  int from_of = -1;
+  auto page_at = [&](int page) __attribute__((always_inline)) {   // of the wave's pages, 2 a unit
+    if (page >> 6 != from_of) {
+      from_of = page >> 6;
+      const int x = min((page & ~63) + lane, 2 * (end - begin) - 1), u = begin + (x >> 1), kind = kind_of(u);
+      const int p = 2 * (u - (kind == kLowPages ? 0 : kind == kHighPages ? u_low : u_high)) + (x & 1);
+      const int id = kind == kWindowPages ? keys.ring_page + min(p, a.cv.ring_pp - 1)
+                     : kind == kLowPages  ? keys.table[0][min(p, (last_sees[0] - 1) >> 4)]
+                                          : keys.table[1][min(p, (last_sees[1] - 1) >> 4)];
+      const uint32_t hs = ((uint32_t)head + (uint32_t)id) % (uint32_t)a.cv.n_kv_heads;
+      const uint64_t at = kind == kLowPages
+                              ? (uint64_t)a.cv.lo_pool + (uint64_t)id * a.cv.lo_page_bytes + hs * (uint32_t)L::kLoHead
+                              : (uint64_t)a.cv.hi_pool + (uint64_t)id * a.cv.hi_page_bytes + hs * (uint32_t)L::kHiHead;
+      from_lo = (uint32_t)at;
+      from_hi = (uint32_t)(at >> 32);
+    }
+    return reinterpret_cast<const uint8_t*>((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)from_hi, page & 63) << 32 |
+                                            (uint32_t)__builtin_amdgcn_readlane((int)from_lo, page & 63));
+  };
+
+  uint4 qf[KI];
+  float scale = 0.0f;                              // of the lane's row, as its queries are held
+  f32x16_t o[VT];
+#pragma unroll
+  for (int m = 0; m < VT; ++m)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[m][r] = 0.0f;
+  float mx = -INFINITY, sum = 0.0f;
+  const uint32_t room = lds_address(s_room[wave]);
+  const long long at = first + (in ? row / G : 0);
+  const int t16 = n & 15, own = n >> 4;            // slot of a page, and which of a unit's two; of values: dimension, parity
+  int u = begin;
+  // The wave's units of one kind up to `to`; u0: the kind's first.
+  auto segment = [&](auto is_low, bool ring, int u0, int to, int fs, int ls, const int32_t* list, int used)
+      __attribute__((always_inline)) {
+    constexpr bool kLow = decltype(is_low)::value;
+    load_queries<kLow, KI>(a, q_row, in, g, qf, scale);
+    // What each row sees: the entries between what the first and the last row see are fewer than the tile's tokens.
+    int sees = fs;
+    if (ls > fs) {
+      const int pos = lane < ls - fs ? list[fs + lane] : INT32_MAX;
+#pragma unroll 1
+      for (int x = 0; x < kFewRows / G; ++x) {
+        const int c = __popcll(__ballot(lane < ls - fs && (long long)pos <= wave_at + x));
+        if (at == wave_at + x) sees = fs + c;
+      }
+    }
+    if (!in) sees = 0;
+    // Copies of page x of the wave's: its bytes `from` .. `from` + kBytes to LDS address `to_lds`.
+    auto copy_page = [&](int x, int from, auto bytes, uint32_t to_lds) __attribute__((always_inline)) {
+      constexpr int kBytes = decltype(bytes)::value;
+      const uint8_t* src = page_at(x) + from;
+#pragma unroll
+      for (int y = 0; y < kBytes; y += 1024)
+        if (y + 1024 <= kBytes || lane * 16 < kBytes - y) copy_to_lds<true>(src, (uint32_t)(y + lane * 16), to_lds + y);
+    };
+    // HIGH: the keys or values of unit v; LOW: the batch of units that starts at v, in half `slot` of the room.
+    auto copy_half = [&](int v, int half) __attribute__((always_inline)) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        copy_page(2 * (v - begin) + h, half * kPart, std::integral_constant<int, kPart>{}, room + (2 * half + h) * kPart);
+    };
+    auto copy_batch = [&](int v, int slot) __attribute__((always_inline)) {
+      for (int x = 0; x < 2 * min(kLowBatch, to - v); ++x)
+        copy_page(2 * (v - begin) + x, 0, std::integral_constant<int, L::kLoHead>{}, room + slot * (kRoom / 2) + x * L::kLoHead);
+    };
+    if constexpr (kLow) {
+      copy_batch(u, 0);
+    } else {
+      copy_half(u, 0);
+      copy_half(u, 1);
+    }
+    int slot = 0;
+#pragma unroll 1
+    while (u < to) {
+      const int batch = kLow ? min(kLowBatch, to - u) : 1, next = u + batch;
+      // What is to be read has arrived; what was asked for behind it may be on its way.
+      if constexpr (kLow) {
+        if (next < to) copy_batch(next, slot ^ 1);
+        if (next + kLowBatch <= to) wait_copies<2 * kLowBatch * ((L::kLoHead + 1023) / 1024)>();
+        else wait_copies<0>();
+      } else {
+        wait_copies<kHalf>();
+      }
+#pragma unroll 1
+      for (int x = 0; x < batch; ++x, ++u) {
+        const int slot0 = 32 * (u - u0);           // the unit's first slot of its store
+        f32x16_t s;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = 0.0f;
+        const int valid = used - slot0;            // of the unit's slots; what was there before is behind them
+        bool wide_keys = false, wide_values = false;   // of a unit with a wide page: taken at 1 / 16
+        const f16x2_t down = {(_Float16)(1.0f / kWide), (_Float16)(1.0f / kWide)};
+        const uint32_t low0 = room + slot * (kRoom / 2) + 2 * x * L::kLoHead;
+        if constexpr (kLow) {
+          // A page's scales are 8 NG words, NG / 2 a slot.
+          const int h = lane / (8 * NG), word = lane % (8 * NG);
+          if (h < 2 && 16 * h + word / (NG / 2) < valid) {
+            const uint32_t ks = read_lds4(low0 + h * L::kLoHead + L::kLoKS + 4 * word);
+            const uint32_t vs = read_lds4(low0 + h * L::kLoHead + L::kLoVS + 4 * word);
+            wide_keys = max(ks & 0xFFFFu, ks >> 16) > kWideScale;
+            wide_values = max(vs & 0xFFFFu, vs >> 16) > kWideScale;
+          }
+          wide_keys = __ballot(wide_keys) != 0ull;
+          wide_values = __ballot(wide_values) != 0ull;
+          const uint32_t k0 = low0 + own * L::kLoHead;
+          uint32_t ks[NG / 2], word0[NG], word1[NG];
+          read_words(k0 + L::kLoKS + t16 * 2 * NG, ks);
+          read_words(k0 + (g * 16 + t16) * 4 * NG, word0);
+          read_words(k0 + ((g + 2) * 16 + t16) * 4 * NG, word1);
+          if (16 * own + t16 >= valid)
+#pragma unroll
+            for (int c = 0; c < NG / 2; ++c) ks[c] = 0u;
+          if (wide_keys)
+#pragma unroll
+            for (int c = 0; c < NG / 2; ++c) ks[c] = word_of(halves(ks[c]) * down);
+#pragma unroll
+          for (int i = 0; i < NG; ++i) {
+            const uint32_t both = __builtin_amdgcn_perm(ks[i / 2], ks[i / 2], i & 1 ? 0x03020302u : 0x01000100u);
+            const f16x2_t s8 = halves(both & 0xFFF8FFF8u), s3 = halves(both) - s8;
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {          // quarters g and g + 2: chunks 2 (2 i + w) + g
+              const uint32_t word = w ? word1[i] : word0[i];
+              const f16x2_t c[4] = {code_pair(word, 0), code_pair(word, 1), code_pair(word, 2), code_pair(word, 3)};
+              s = mfma_half(make_uint4(word_of(c[0] * s8), word_of(c[1] * s8), word_of(c[2] * s8), word_of(c[3] * s8)),
+                            qf[2 * i + w], s);
+              s = mfma_half(make_uint4(word_of(c[0] * s3), word_of(c[1] * s3), word_of(c[2] * s3), word_of(c[3] * s3)),
+                            qf[2 * i + w], s);
+            }
+          }
+          if (wide_keys) s *= kWide;
+        } else {
+          const uint32_t k0 = fresh(room + own * kPart + g * 256 + t16 * 16);
+#pragma unroll
+          for (int k = 0; k < KI; ++k) s = mfma(read_lds16(k0 + 512 * k), qf[k], s);
+          lds_barrier_wave();                      // the keys have been read: the next unit's may come
+          if (next < to) copy_half(next, 0);
+        }
+        // The value operands of a HIGH page h.
+        const uint32_t v0 = fresh(room + 2 * kPart + g * 256 + t16 * 16 + own * 8), v1 = fresh(v0 + 512);
+        auto high_value = [&](int h, int m) {
+          const u32x2_t y = *(const lds_u32x2*)(uintptr_t)(v0 + h * kPart + m * 1024);
+          const u32x2_t z = *(const lds_u32x2*)(uintptr_t)(v1 + h * kPart + m * 1024);
+          return make_uint4(y[0], y[1], z[0], z[1]);
+        };
+        auto both = [&](int t) { return (t < valid ? 0xFFFFu : 0u) | (t + 1 < valid ? 0xFFFF0000u : 0u); };
+        auto used_value = [&](int h, int m) {      // slots behind the last entry as 0
+          const uint4 v = high_value(h, m);
+          const int t = 16 * h + 4 * g;
+          return make_uint4(v.x & both(t), v.y & both(t + 2), v.z & both(t + 8), v.w & both(t + 10));
+        };
+        const bool edge = ring || fs < slot0 + 32;
+        uint32_t hidden = 0u;
+        if (edge) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int k = slot0 + 8 * (r >> 2) + 4 * g + (r & 3);
+            const bool hid = ring ? !in || ring_position(keys, a.cv.window, k) > at : k >= sees;
+            hidden |= (uint32_t)hid << r;
+            s[r] = hid ? -INFINITY : s[r];
+          }
+        }
+        float top = fmaxf(s[0], s[1]);
+#pragma unroll
+        for (int r = 2; r < 16; ++r) top = fmaxf(top, s[r]);
+        top = fmaxf(top, __shfl_xor(top, 32));
+        top = top == -INFINITY ? top : top * scale;
+        if (__ballot(top > mx + kHeadroom)) {      // the reference follows a maximum that exceeds it
+          const float ref = top > mx + kHeadroom ? top - kBelow : mx;
+          const float alpha = ref == mx ? 1.0f : __builtin_amdgcn_exp2f(mx - ref);
+          sum *= alpha;
+#pragma unroll
+          for (int m = 0; m < VT; ++m) o[m] *= alpha;
+          mx = ref;
+        }
+        const float base = mx == -INFINITY ? 0.0f : mx;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const float w = __builtin_amdgcn_exp2f(fmaf(s[r], scale, -base));
+          s[r] = hidden >> r & 1u ? 0.0f : w;
+          sum += s[r];
+        }
+        if constexpr (kLow) {
+          if (wide_values)
+#pragma unroll
+            for (int m = 0; m < VT; ++m) o[m] *= 1.0f / kWide;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            uint32_t v[VT][4];
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {          // slots 4 g .. and 4 g + 8 .., the parity's nibbles
+              uint32_t vs[2 * NG], code[NG];
+              read_words(low0 + h * L::kLoHead + L::kLoVS + (g + 2 * w) * 8 * NG, vs);
+              read_words(low0 + h * L::kLoHead + L::kLoVC + ((g + 2 * w) * 16 + t16) * 4 * NG, code);
+              if (valid < 32)
+#pragma unroll
+                for (int c = 0; c < 2 * NG; ++c)
+                  if (16 * h + 4 * (g + 2 * w) + c / (NG / 2) >= valid) vs[c] = 0u;
+              if (wide_values)
+#pragma unroll
+                for (int c = 0; c < 2 * NG; ++c) vs[c] = word_of(halves(vs[c]) * down);
+#pragma unroll
+              for (int m = 0; m < VT; ++m) {
+                const uint32_t pick = m & 1 ? 0x07060302u : 0x05040100u;
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+                  v[m][2 * w + t] = word_of(code_pair(code[m] >> (4 * own), t) *
+                                            halves(__builtin_amdgcn_perm(vs[(t + 2) * (NG / 2) + m / 2], vs[t * (NG / 2) + m / 2], pick)));
+              }
+            }
+            const uint4 p = packed_weights<true>(s, h);
+#pragma unroll
+            for (int m = 0; m < VT; ++m) o[m] = mfma_half(make_uint4(v[m][0], v[m][1], v[m][2], v[m][3]), p, o[m]);
+          }
+          if (wide_values)
+#pragma unroll
+            for (int m = 0; m < VT; ++m) o[m] *= kWide;
+        } else {
+          if (next < to) wait_copies<kHalf>();
+          else wait_copies<0>();
+          bool wild = false;                       // at the edge, some value is infinite or NaN
+          if (edge)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+              for (int m = 0; m < VT; ++m) wild |= abs_max_bits8(used_value(h, m)) >= 0x7F80u;
+          if (__ballot(wild)) {
+            const uint8_t* values = s_room[wave] + 2 * kPart;
+            add_seen_values<VT>(values, values + kPart, s, hidden, o, g, n);
+          } else {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const uint4 p = packed_weights<false>(s, h);
+#pragma unroll
+              for (int m = 0; m < VT; ++m) o[m] = mfma(edge ? used_value(h, m) : high_value(h, m), p, o[m]);
+            }
+          }
+          lds_barrier_wave();
+          if (next < to) copy_half(next, 1);
+        }
+      }
+      slot ^= 1;
+      lds_barrier_wave();                          // the batch has been read
+    }
+  };
+  if (u < min(u_low, end)) segment(std::true_type{}, false, 0, min(u_low, end), first_sees[0], last_sees[0], keys.list[0], keys.n[0]);
+#pragma unroll 1
+  for (int k = 0; k < 2; ++k) {                    // HIGH entries, then the window's
+    const int to = k ? end : min(u_high, end);
+    if (u >= to) continue;
+    segment(std::false_type{}, k == 1, k ? u_high : u_low, to, k ? 0 : first_sees[1], k ? 0 : last_sees[1], keys.list[1],
+            k ? keys.ring_slots : keys.n[1]);
+  }
+  sum += __shfl_xor(sum, 32);
+
+  // The waves' sums joined: row x's output d at float (d + 4 x) mod D of its row, so that the stores of 32 rows do not
+  // meet on the same banks.
+  lds_barrier();
+  float* mine = reinterpret_cast<float*>(s_room[wave]) + n * D;
+#pragma unroll
+  for (int m = 0; m < VT; ++m)
+#pragma unroll
+    for (int r = 0; r < 16; r += 4)
+      *reinterpret_cast<float4*>(mine + ((32 * m + 2 * r + 4 * g + 4 * n) & (D - 1))) =
+          make_float4(o[m][r], o[m][r + 1], o[m][r + 2], o[m][r + 3]);
+  if (g == 0) s_ml[wave][n] = make_float2(mx, sum);
+  __syncthreads();
+  constexpr int kEach = kFewRows * D / (64 * kFewWaves);     // outputs of a thread: 16 or 8 of one row
+  const int x = (int)threadIdx.x * kEach / D, d0 = (int)threadIdx.x * kEach % D;
+  float ref = -INFINITY, total = 0.0f, acc[kEach];
+#pragma unroll
+  for (int w = 0; w < kFewWaves; ++w) ref = fmaxf(ref, s_ml[w][x].x);
+#pragma unroll
+  for (int d = 0; d < kEach; ++d) acc[d] = 0.0f;
+#pragma unroll
+  for (int w = 0; w < kFewWaves; ++w) {
+    const float2 ml = s_ml[w][x];
+    if (ml.y == 0.0f) continue;
+    const float f = __builtin_amdgcn_exp2f(ml.x - ref);
+    total = fmaf(ml.y, f, total);
+#pragma unroll
+    for (int d = 0; d < kEach; d += 4) {
+      const float4 v = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(s_room[w]) + x * D +
+                                                        ((d0 + d + 4 * x) & (D - 1)));
+      acc[d] = fmaf(v.x, f, acc[d]);
+      acc[d + 1] = fmaf(v.y, f, acc[d + 1]);
+      acc[d + 2] = fmaf(v.z, f, acc[d + 2]);
+      acc[d + 3] = fmaf(v.w, f, acc[d + 3]);
+    }
+  }
+  const int to = row0 + x;
+  if (to >= n_rows) return;
+  if (a.pieces > 1) {
+    const size_t w = (((size_t)b * a.cv.n_kv_heads + head) * a.pieces + piece) * ((size_t)a.max_q * G) + to;
+#pragma unroll
+    for (int d = 0; d < kEach; d += 4)
+      *reinterpret_cast<float4*>(a.ws_o + w * D + d0 + d) = make_float4(acc[d], acc[d + 1], acc[d + 2], acc[d + 3]);
+    if (d0 == 0) *reinterpret_cast<float2*>(a.ws_ml + 2 * w) = make_float2(ref, total);
+    return;
+  }
+  const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+  const size_t w = ((size_t)b * a.max_q + to / G) * a.n_q_heads + (size_t)head * G + to % G;
+#pragma unroll
+  for (int d = 0; d < kEach; d += 4)
+    *reinterpret_cast<uint2*>(a.out + w * D + d0 + d) =
+        make_uint2(pack_bf16x2(acc[d] * inv, acc[d + 1] * inv), pack_bf16x2(acc[d + 2] * inv, acc[d + 3] * inv));
+  if (a.lse && d0 == 0) a.lse[w] = total == 0.0f ? -INFINITY : (ref + __builtin_amdgcn_logf(total)) * kLn2;
+}
+
+// Joins the pieces of a row: the parts' sums and outputs, taken to the largest
+// of their references.  kWaves waves take every kWaves-th piece of a row; a
+// workgroup takes 4 / kWaves rows.
+template <int D, int G, int kWaves>
 __global__ __launch_bounds__(256) void prompt_merge_kernel(PromptArgs a) {
-  const int lane = (int)threadIdx.x & 63;
-  const int64_t x = (int64_t)blockIdx.x * 4 + ((int)threadIdx.x >> 6), rows = (int64_t)a.max_q * G;
+  __shared__ float s_o[4][D];
+  __shared__ float2 s_ml[4];
+  constexpr int E = D / 64;
+  const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int64_t x = (int64_t)blockIdx.x * (4 / kWaves) + wave / kWaves, rows = (int64_t)a.max_q * G;
   const int64_t bh = x / rows;
   const int row = (int)(x - bh * rows), b = (int)(bh / a.cv.n_kv_heads), head = (int)(bh % a.cv.n_kv_heads);
-  if (b >= a.batch) return;
-  const int nq = a.n_q ? min(a.n_q[b], a.max_q) : a.max_q;
-  if (row >= nq * G) return;
+  const bool live = b < a.batch && row < (a.n_q ? min(a.n_q[b], a.max_q) : a.max_q) * G;
   const size_t first = (size_t)bh * a.pieces * rows + row;
-  float top = -INFINITY;
-  for (int p = 0; p < a.pieces; ++p) top = fmaxf(top, a.ws_ml[2 * (first + (size_t)p * rows)]);
-  float sum = 0.0f, o[D / 64];
+  float top = -INFINITY, sum = 0.0f, o[E];
 #pragma unroll
-  for (int d = 0; d < D / 64; ++d) o[d] = 0.0f;
-  for (int p = 0; p < a.pieces; ++p) {
-    const size_t at = first + (size_t)p * rows;
-    const float2 ml = *reinterpret_cast<const float2*>(a.ws_ml + 2 * at);
-    if (ml.y == 0.0f) continue;                    // a piece of which the row sees nothing
-    const float w = __builtin_amdgcn_exp2f(ml.x - top);
-    sum = fmaf(ml.y, w, sum);
+  for (int d = 0; d < E; ++d) o[d] = 0.0f;
+  if (live) {
+    // 64 pieces at a time, references and sums one per lane.
+    for (int p0 = wave % kWaves; p0 < a.pieces; p0 += 64 * kWaves) {
+      const int mine = p0 + lane * kWaves, n = min(64, (a.pieces - p0 + kWaves - 1) / kWaves);
+      const float2 ml = lane < n ? *reinterpret_cast<const float2*>(a.ws_ml + 2 * (first + (size_t)mine * rows))
+                                 : make_float2(-INFINITY, 0.0f);
+      float ref = ml.x;
 #pragma unroll
-    for (int d = 0; d < D / 64; ++d) o[d] = fmaf(a.ws_o[at * D + lane * (D / 64) + d], w, o[d]);
+      for (int s = 1; s < 64; s *= 2) ref = fmaxf(ref, __shfl_xor(ref, s));
+      ref = fmaxf(ref, top);
+      const float keep = top == ref ? 1.0f : __builtin_amdgcn_exp2f(top - ref);
+      const float w = ml.y == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(ml.x - ref);   // 0: the row sees nothing of the piece
+      float part = ml.y == 0.0f ? 0.0f : ml.y * w;
+#pragma unroll
+      for (int s = 1; s < 64; s *= 2) part += __shfl_xor(part, s);
+      sum = fmaf(sum, keep, part);
+#pragma unroll
+      for (int d = 0; d < E; ++d) o[d] *= keep;
+      top = ref;
+#pragma unroll 8
+      for (int p = 0; p < n; ++p) {
+        const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), p));
+        if (f == 0.0f) continue;
+        const float* from = a.ws_o + (first + (size_t)(p0 + p * kWaves) * rows) * D + lane * E;
+#pragma unroll
+        for (int d = 0; d < E; ++d) o[d] = fmaf(from[d], f, o[d]);
+      }
+    }
   }
+  if (kWaves > 1) {
+#pragma unroll
+    for (int d = 0; d < E; ++d) s_o[wave][lane * E + d] = o[d];
+    if (lane == 0) s_ml[wave] = make_float2(top, sum);
+    __syncthreads();
+    if (wave) return;
+    float ref = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) ref = fmaxf(ref, s_ml[w].x);
+    sum = 0.0f;
+#pragma unroll
+    for (int d = 0; d < E; ++d) o[d] = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      if (s_ml[w].y == 0.0f) continue;
+      const float f = __builtin_amdgcn_exp2f(s_ml[w].x - ref);
+      sum = fmaf(s_ml[w].y, f, sum);
+#pragma unroll
+      for (int d = 0; d < E; ++d) o[d] = fmaf(s_o[w][lane * E + d], f, o[d]);
+    }
+    top = ref;
+  }
+  if (!live) return;
   const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
   const size_t to = ((size_t)b * a.max_q + row / G) * a.n_q_heads + (size_t)head * G + row % G;
   if constexpr (D == 128) {
@@ -698,10 +1150,12 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(PromptArgs a) {
 template <int D, int G>
 void launch_group(const PromptArgs& a, const PromptCut& c, hipStream_t s) {
   const dim3 blocks((unsigned)prompt_blocks(a, c));
-  prompt_kernel<D, G, 8><<<blocks, dim3(512), 0, s>>>(a);
+  if (c.rows == kFewRows) prompt_few_kernel<D, G><<<blocks, dim3(64 * kFewWaves), 0, s>>>(a);
+  else prompt_kernel<D, G, 8><<<blocks, dim3(512), 0, s>>>(a);
   if (a.pieces > 1) {
     const int64_t rows = (int64_t)a.batch * a.cv.n_kv_heads * a.max_q * G;
-    prompt_merge_kernel<D, G><<<dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s>>>(a);
+    if (a.pieces > 8) prompt_merge_kernel<D, G, 4><<<dim3((unsigned)rows), dim3(256), 0, s>>>(a);
+    else prompt_merge_kernel<D, G, 1><<<dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s>>>(a);
   }
 }
 
@@ -717,14 +1171,20 @@ void launch_dim(const PromptArgs& a, const PromptCut& c, hipStream_t s) {
 
 }  // namespace
 
-// Tiles of 256 rows (eight waves share every page through LDS).  The keys are
-// cut where the tiles leave compute units idle, into pieces of at least 256.
+// Tiles of 256 rows, whose eight waves share every page through LDS, or of 32,
+// whose waves share the rows, where no sequence has more than kFewMost.  The keys
+// are cut into pieces where the tiles leave compute units idle.
 PromptCut prompt_cut(int32_t batch, int32_t max_q, int32_t group, int32_t n_kv_heads, int32_t max_ctx_hint) {
   PromptCut c;
   const int64_t rows = (int64_t)max_q * group;
-  c.rows = 256;
+  c.rows = rows <= kFewMost ? kFewRows : 256;
   const int64_t tiles = (rows + c.rows - 1) / c.rows * batch * n_kv_heads;
-  c.pieces = (int32_t)std::max<int64_t>(1, std::min<int64_t>(256 / tiles, (max_ctx_hint + 255) / 256));
+  if (c.rows == kFewRows) {                        // of 4 waves each, with a unit or more for each wave
+    const int64_t want = tiles < 128 ? 512 : 1024;
+    c.pieces = (int32_t)std::max<int64_t>(1, std::min<int64_t>((want + tiles - 1) / tiles, (max_ctx_hint + 127) / 128));
+  } else {
+    c.pieces = (int32_t)std::max<int64_t>(1, std::min<int64_t>(256 / tiles, (max_ctx_hint + 255) / 256));
+  }
   return c;
 }
 
