@@ -904,12 +904,6 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void prompt_few_kernel(PromptArg
           const u32x2_t z = *(const lds_u32x2*)(uintptr_t)(v1 + h * kPart + m * 1024);
           return make_uint4(y[0], y[1], z[0], z[1]);
         };
-        auto both = [&](int t) { return (t < valid ? 0xFFFFu : 0u) | (t + 1 < valid ? 0xFFFF0000u : 0u); };
-        auto used_value = [&](int h, int m) {      // slots behind the last entry as 0
-          const uint4 v = high_value(h, m);
-          const int t = 16 * h + 4 * g;
-          return make_uint4(v.x & both(t), v.y & both(t + 2), v.z & both(t + 8), v.w & both(t + 10));
-        };
         const bool edge = ring || fs < slot0 + 32;
         uint32_t hidden = 0u;
         if (edge) {
@@ -980,11 +974,20 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void prompt_few_kernel(PromptArg
           if (next < to) wait_copies<kHalf>();
           else wait_copies<0>();
           bool wild = false;                       // at the edge, some value is infinite or NaN
-          if (edge)
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-              for (int m = 0; m < VT; ++m) wild |= abs_max_bits8(used_value(h, m)) >= 0x7F80u;
+          if (edge) {
+            // Slots behind the last entry hold what was there before: made 0 in LDS, where 16 bytes hold 4 slots twice.
+            const uint32_t values = room + 2 * kPart + lane * 16;
+#pragma unroll 1
+            for (int c = 0; c < kHalf; ++c) {
+              const int t = 16 * (c / (kHalf / 2)) + 4 * (lane >> 4);
+              const uint32_t lo = (t < valid ? 0xFFFFu : 0u) | (t + 1 < valid ? 0xFFFF0000u : 0u);
+              const uint32_t hi = (t + 2 < valid ? 0xFFFFu : 0u) | (t + 3 < valid ? 0xFFFF0000u : 0u);
+              uint4 v = read_lds16(values + c * 1024);
+              v = make_uint4(v.x & lo, v.y & hi, v.z & lo, v.w & hi);
+              if (valid < 32) write_lds16(values + c * 1024, v);
+              wild |= abs_max_bits8(v) >= 0x7F80u;
+            }
+          }
           if (__ballot(wild)) {
             const uint8_t* values = s_room[wave] + 2 * kPart;
             add_seen_values<VT>(values, values + kPart, s, hidden, o, g, n);
@@ -993,7 +996,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void prompt_few_kernel(PromptArg
             for (int h = 0; h < 2; ++h) {
               const uint4 p = packed_weights<false>(s, h);
 #pragma unroll
-              for (int m = 0; m < VT; ++m) o[m] = mfma(edge ? used_value(h, m) : high_value(h, m), p, o[m]);
+              for (int m = 0; m < VT; ++m) o[m] = mfma(high_value(h, m), p, o[m]);
             }
           }
           lds_barrier_wave();
