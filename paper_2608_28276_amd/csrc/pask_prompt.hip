@@ -740,15 +740,12 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void prompt_few_kernel(PromptArg
   const bool in = row < n_rows;
   const Keys keys = keys_of(a.cv, b, a.layer);
   const long long first = a.first ? (long long)a.first[b] : (long long)keys.n_pos - nq;
-  // Entries of each list that the first row sees, and the last.
+  // Entries of each list that the first row sees, and the last: 16 lanes for each of the four.
   const long long wave_at = first + row0 / G, wave_end = first + (min(row0 + kFewRows, n_rows) - 1) / G;
-  int first_sees[2], last_sees[2];
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const int seen = entries_at(keys.list[k], keys.n[k], keys.n_pos, lane < 32 ? wave_at : wave_end);
-    first_sees[k] = __builtin_amdgcn_readlane(seen, 0);
-    last_sees[k] = __builtin_amdgcn_readlane(seen, 32);
-  }
+  const int seen = entries_at(lane < 32 ? keys.list[0] : keys.list[1], lane < 32 ? keys.n[0] : keys.n[1], keys.n_pos,
+                              lane & 16 ? wave_end : wave_at);
+  const int first_sees[2] = {__builtin_amdgcn_readlane(seen, 0), __builtin_amdgcn_readlane(seen, 32)};
+  const int last_sees[2] = {__builtin_amdgcn_readlane(seen, 16), __builtin_amdgcn_readlane(seen, 48)};
   const bool ring_seen = keys.ring_slots > 0 && wave_end >= (long long)keys.n_pos - keys.ring_slots;
   const int u_low = (last_sees[0] + 31) / 32, u_high = u_low + (last_sees[1] + 31) / 32;
   const int units = u_high + (ring_seen ? (keys.ring_slots + 31) / 32 : 0);
@@ -795,18 +792,6 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void prompt_few_kernel(PromptArg
   auto segment = [&](auto is_low, bool ring, int u0, int to, int fs, int ls, const int32_t* list, int used)
       __attribute__((always_inline)) {
     constexpr bool kLow = decltype(is_low)::value;
-    load_queries<kLow, KI>(a, q_row, in, g, qf, scale);
-    // What each row sees: the entries between what the first and the last row see are fewer than the tile's tokens.
-    int sees = fs;
-    if (ls > fs) {
-      const int pos = lane < ls - fs ? list[fs + lane] : INT32_MAX;
-#pragma unroll 1
-      for (int x = 0; x < kFewRows / G; ++x) {
-        const int c = __popcll(__ballot(lane < ls - fs && (long long)pos <= wave_at + x));
-        if (at == wave_at + x) sees = fs + c;
-      }
-    }
-    if (!in) sees = 0;
     // Copies of page x of the wave's: its bytes `from` .. `from` + kBytes to LDS address `to_lds`.
     auto copy_page = [&](int x, int from, auto bytes, uint32_t to_lds) __attribute__((always_inline)) {
       constexpr int kBytes = decltype(bytes)::value;
@@ -831,6 +816,18 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void prompt_few_kernel(PromptArg
       copy_half(u, 0);
       copy_half(u, 1);
     }
+    load_queries<kLow, KI>(a, q_row, in, g, qf, scale);
+    // What each row sees: the entries between what the first and the last row see are fewer than the tile's tokens.
+    int sees = fs;
+    if (ls > fs) {
+      const int pos = lane < ls - fs ? list[fs + lane] : INT32_MAX;
+#pragma unroll 1
+      for (int x = 0; x < kFewRows / G; ++x) {
+        const int c = __popcll(__ballot(lane < ls - fs && (long long)pos <= wave_at + x));
+        if (at == wave_at + x) sees = fs + c;
+      }
+    }
+    if (!in) sees = 0;
     int slot = 0;
 #pragma unroll 1
     while (u < to) {

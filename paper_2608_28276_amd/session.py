@@ -131,11 +131,14 @@ class PaskSession:
         if m == 0:
             return
         hint = max_ctx_hint or self.max_ctx_hint
-        with torch.cuda.device(buf):
-            need = prompt.pask_prompt_workspace_bytes(g, b, m, hint)
-            ws = torch.empty(need, dtype=torch.uint8, device=buf) if need else None
-            prompt.pask_prompt_attn(self.cache, layer, b, m, n_q, first, q, out, lse, self.softmax_scale, hint, ws, need,
-                                    self.stream)
+        need = prompt.pask_prompt_workspace_bytes(g, b, m, hint)
+        ws = torch.empty(need, dtype=torch.uint8, device=buf) if need else None
+        args = (self.cache, layer, b, m, n_q, first, q, out, lse, self.softmax_scale, hint, ws, need)
+        if torch.cuda.current_device() == buf.index:
+            prompt.pask_prompt_attn(*args, self.stream)
+        else:
+            with torch.cuda.device(buf):
+                prompt.pask_prompt_attn(*args, self.stream)
 
     def budgets(self):
         """Remaining budget R of every (sequence, layer), int64 [max_batch, n_layers]."""
