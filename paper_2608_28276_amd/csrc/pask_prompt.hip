@@ -1173,17 +1173,32 @@ void launch_dim(const PromptArgs& a, const PromptCut& c, hipStream_t s) {
 
 // Tiles of 256 rows, whose eight waves share every page through LDS, or of 32,
 // whose waves share the rows, where no sequence has more than kFewMost.  The keys
-// are cut into pieces where the tiles leave compute units idle.
-PromptCut prompt_cut(int32_t batch, int32_t max_q, int32_t group, int32_t n_kv_heads, int32_t max_ctx_hint) {
+// are cut into pieces where the tiles leave compute units idle.  For tiles of 256
+// rows by what a call takes with each number of pieces, in microseconds: as many
+// turns of the 256 compute units as the workgroups need, each a piece's steps at
+// 2.5 (64 keys: 2.1 of bf16 pages, 3.2 of int4 ones) and 10 to begin and end, and
+// the joining, 6 and its traffic (88 tiles of 32,333 tokens, most of them int4:
+// 509 with 2 pieces, PIECES with the 8 of this rule).
+PromptCut prompt_cut(int32_t batch, int32_t max_q, int32_t group, int32_t n_kv_heads, int32_t head_dim,
+                     int32_t max_ctx_hint) {
   PromptCut c;
   const int64_t rows = (int64_t)max_q * group;
   c.rows = rows <= kFewMost ? kFewRows : 256;
+  c.pieces = 1;
   const int64_t tiles = (rows + c.rows - 1) / c.rows * batch * n_kv_heads;
   if (c.rows == kFewRows) {                        // of 4 waves each, with a unit or more for each wave
     const int64_t want = tiles < 128 ? 512 : 1024;
     c.pieces = (int32_t)std::max<int64_t>(1, std::min<int64_t>((want + tiles - 1) / tiles, (max_ctx_hint + 127) / 128));
-  } else {
-    c.pieces = (int32_t)std::max<int64_t>(1, std::min<int64_t>(256 / tiles, (max_ctx_hint + 255) / 256));
+    return c;
+  }
+  const double steps = (max_ctx_hint + kStepKeys - 1) / kStepKeys, traffic = 2.0 * 4 * head_dim * c.rows * 1e-6 / 4.0;
+  double least = 0.0;
+  for (int32_t p = 1; p == 1 || (p <= 32 && p * tiles <= 1024 && 4 * p <= steps); ++p) {
+    double t = (double)((tiles * p + 255) / 256) * (2.5 * steps / p + 10.0);
+    if (p > 1) t += 6.0 + traffic * (double)(tiles * p);
+    if (p > 1 && t >= least) continue;
+    least = t;
+    c.pieces = p;
   }
   return c;
 }

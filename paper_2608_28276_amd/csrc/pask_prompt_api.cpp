@@ -48,7 +48,7 @@ int32_t hint_of(const pask_geom& g, int32_t max_ctx_hint) {
 }
 
 pask::PromptCut cut_of(const pask_geom& g, int32_t batch, int32_t max_q, int32_t max_ctx_hint) {
-  return pask::prompt_cut(batch, max_q, g.n_q_heads / g.n_kv_heads, g.n_kv_heads, hint_of(g, max_ctx_hint));
+  return pask::prompt_cut(batch, max_q, g.n_q_heads / g.n_kv_heads, g.n_kv_heads, g.head_dim, hint_of(g, max_ctx_hint));
 }
 
 struct WsLayout {

@@ -50,7 +50,8 @@ struct PromptArgs {
 struct PromptCut {
   int32_t rows, pieces;
 };
-PromptCut prompt_cut(int32_t batch, int32_t max_q, int32_t group, int32_t n_kv_heads, int32_t max_ctx_hint);
+PromptCut prompt_cut(int32_t batch, int32_t max_q, int32_t group, int32_t n_kv_heads, int32_t head_dim,
+                     int32_t max_ctx_hint);
 int64_t prompt_blocks(const PromptArgs& a, const PromptCut& c);   // workgroups of the attention kernel
 
 hipError_t launch_prompt(const PromptArgs& a, const PromptCut& c, hipStream_t s);
