@@ -111,6 +111,19 @@ __device__ __forceinline__ f16x2_t code_pair(uint32_t w, int x) {
   return halves(n | 0x64006400u) - halves(0x64086408u);
 }
 
+// The same pairs as 16 + code + 8 (its last bit at 1 / 64): times a scale of 8
+// bits or fewer, less 24 scales (24 has 2 bits, fp16 11), is exact.
+__device__ __forceinline__ f16x2_t raised_pair(uint32_t w, int x) {
+  const uint32_t n = (x == 0 ? w << 6 : x == 1 ? w >> 2 : x == 2 ? w << 2 : w >> 6) & 0x03C003C0u;
+  return halves(n | 0x4C004C00u);
+}
+// A key's 8 codes times a scale pair.
+__device__ __forceinline__ uint4 key_part(uint32_t w, f16x2_t s) {
+  const f16x2_t s24 = s * (f16x2_t){(_Float16)-24.0f, (_Float16)-24.0f};
+  auto pair = [&](int x) { return word_of(__builtin_elementwise_fma(raised_pair(w, x), s, s24)); };
+  return make_uint4(pair(0), pair(1), pair(2), pair(3));
+}
+
 // Codes and scales of one thread's share of a LOW page: quarter q of slot t's
 // key (NG words of 8 elements, slot t's NG scales), or 4 slots of NG pairs of
 // dimensions (e + 32 i, + 16) of the values (4 slots' NG scales).
@@ -120,10 +133,10 @@ struct LowPart {
   uint32_t code[NG];
   uint32_t scale[2 * NG];                          // keys: the first NG / 2
 };
-// A page with a scale above this (fp16 bits of 65504 / 7, rounded down) holds elements that fp16 does not; it is taken
-// at 1 / 16 of them.
-constexpr uint32_t kWideScale = 0x7091u;
-constexpr float kWide = 16.0f;
+// A page with a scale above this (fp16 bits of 2728) is taken at 1 / 32 of its
+// elements: 24 scales, and 7, are below the largest fp16.
+constexpr uint32_t kWideScale = 0x6954u;
+constexpr float kWide = 32.0f;
 
 // O += P V key by key over 32 keys (values of pages at v0 and v1), where a value
 // that some query does not see is infinite or NaN (a weight of 0 times it is
@@ -266,7 +279,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
   // A page in LDS: keys, the rest of LOW keys, values.
   constexpr int kPart = L::kHiV, kValues = 2 * kPart, kTile = 3 * kPart, kStep = kStepPages * kTile;
   __shared__ __align__(1024) uint8_t s_kv[3][kStep];
-  __shared__ __align__(16) uint32_t s_wide[3][2 * kStepPages];   // LOW parts (keys, values of a page) at 1 / 16
+  __shared__ __align__(16) uint32_t s_wide[3][2 * kStepPages];   // LOW parts (keys, values of a page) at 1 / 32
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int g = lane >> 5, n = lane & 31;
   // Workgroups go to the 8 XCDs in turn: neighbours are different KV heads.  The
@@ -413,10 +426,8 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
           const uint32_t both = __builtin_amdgcn_perm(sc[i / 2], sc[i / 2], pick), upper = both & 0xFFF8FFF8u;
           const f16x2_t s8 = halves(upper), s3 = halves(both) - s8;
           const uint32_t w = low[k].code[i];
-          const f16x2_t c[4] = {code_pair(w, 0), code_pair(w, 1), code_pair(w, 2), code_pair(w, 3)};
-          write_lds16(at + i * 1024, make_uint4(word_of(c[0] * s8), word_of(c[1] * s8), word_of(c[2] * s8), word_of(c[3] * s8)));
-          write_lds16(at + kPart + i * 1024,
-                      make_uint4(word_of(c[0] * s3), word_of(c[1] * s3), word_of(c[2] * s3), word_of(c[3] * s3)));
+          write_lds16(at + i * 1024, key_part(w, s8));
+          write_lds16(at + kPart + i * 1024, key_part(w, s3));
         }
       }
     }
@@ -847,7 +858,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void prompt_few_kernel(PromptArg
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] = 0.0f;
         const int valid = used - slot0;            // of the unit's slots; what was there before is behind them
-        bool wide_keys = false, wide_values = false;   // of a unit with a wide page: taken at 1 / 16
+        bool wide_keys = false, wide_values = false;   // of a unit with a wide page: taken at 1 / 32
         const f16x2_t down = {(_Float16)(1.0f / kWide), (_Float16)(1.0f / kWide)};
         const uint32_t low0 = room + slot * (kRoom / 2) + 2 * x * L::kLoHead;
         if constexpr (kLow) {
@@ -879,11 +890,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void prompt_few_kernel(PromptArg
 #pragma unroll
             for (int w = 0; w < 2; ++w) {          // quarters g and g + 2: chunks 2 (2 i + w) + g
               const uint32_t word = w ? word1[i] : word0[i];
-              const f16x2_t c[4] = {code_pair(word, 0), code_pair(word, 1), code_pair(word, 2), code_pair(word, 3)};
-              s = mfma_half(make_uint4(word_of(c[0] * s8), word_of(c[1] * s8), word_of(c[2] * s8), word_of(c[3] * s8)),
-                            qf[2 * i + w], s);
-              s = mfma_half(make_uint4(word_of(c[0] * s3), word_of(c[1] * s3), word_of(c[2] * s3), word_of(c[3] * s3)),
-                            qf[2 * i + w], s);
+              s = mfma_half(key_part(word, s8), qf[2 * i + w], s);
+              s = mfma_half(key_part(word, s3), qf[2 * i + w], s);
             }
           }
           if (wide_keys) s *= kWide;
@@ -928,9 +936,15 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void prompt_few_kernel(PromptArg
         const float base = mx == -INFINITY ? 0.0f : mx;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          const float w = __builtin_amdgcn_exp2f(fmaf(s[r], scale, -base));
-          s[r] = hidden >> r & 1u ? 0.0f : w;
-          sum += s[r];
+          s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale, -base));
+          if (!edge) sum += s[r];
+        }
+        if (edge) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            s[r] = hidden >> r & 1u ? 0.0f : s[r];
+            sum += s[r];
+          }
         }
         if constexpr (kLow) {
           if (wide_values)

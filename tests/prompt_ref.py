@@ -10,8 +10,8 @@ weight.  To an output's bound come
                  2^8 or more, as the reference lies 8 under a maximum: an entry's
                  weight lacks 2^-33 of the largest at most, and the sum that
                  divides it is no less than the largest
-  2^-21          where a value is above 65504: the values of its page are taken
-                 at 1 / 16, where fp16 rounds by 2^-25 at least
+  2^-20          where a value is above 19,096 (a scale above 2728): the values of
+                 its page are taken at 1 / 32, where fp16 rounds by 2^-25 at least
 
 Rotary bounds: an element x cos a - y sin a is off by half a step of bf16
 (2^-8 of it) and by (|x| + |y|) m times
@@ -89,7 +89,7 @@ def prompt(cache, b, q, first, scale):
             out[:, h], lse[:, h], out_tol[:, h], lse_tol[:, h] = latent_ref.attention(q[:, h], k[:, g], v[:, g], scale,
                                                                                       seen)
             out_tol[:, h] += 2.0 ** -33 * (seen @ np.abs(v[:, g]))
-        out_tol += 2.0 ** -21 * bool((np.abs(v) > 65504).any())
+        out_tol += 2.0 ** -20 * bool((np.abs(v) > 19096).any())
     return out, lse, out_tol, lse_tol
 
 

@@ -208,7 +208,18 @@ def test_hidden_values_that_are_not_finite(value, n_q, window):
     assert not np.isfinite(f64(out[0, m:, 2:, 7])).any()      # heads 2 and 3 read KV head 1
 
 
-@pytest.mark.parametrize("gain", [2.0 ** -12, 2.0 ** 14, 2.0 ** 17])
+@pytest.mark.parametrize("gain", [2.0 ** 11, 2.0 ** 13, 2.0 ** 15])
+def test_int4_keys_of_any_size(gain):
+    """Keys whose scales 24 of which fp16 does not hold, beside ordinary ones; a key enters as before but for fp16's
+    2^-20 in pages with a scale above 2728 (the bound: scale 2^-20 sum |q|, twice for the weights)."""
+    r = Run(2, 4, 2, 128, 900, (LOW,), seed=33)
+    for n, factor in ((200, 1.0), (64, gain), (130, 1.0), (100, gain)):
+        r.append([n, n // 2], k=normal(r.gen, 2, n, 2, 128) * factor)
+    r.attend([100, 50], what="keys", scale=2.0 ** -13)
+    r.attend([5, 5], what="keys", scale=2.0 ** -13)
+
+
+@pytest.mark.parametrize("gain", [2.0 ** -12, 2.0 ** 12, 2.0 ** 14, 2.0 ** 17])
 def test_int4_values_of_any_size(gain):
     """Values down to fp16's subnormals and beyond its range, in pages of their own and beside ordinary ones."""
     r = Run(2, 4, 2, 128, 900, (LOW,), seed=17)
