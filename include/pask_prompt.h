@@ -90,7 +90,8 @@ int pask_rope_init(pask_rope* out, int32_t head_dim, int32_t rot_first, int32_t 
  * and behind are neither read nor written.
  *
  * Errors: PASK_E_ARG (null rope or a rope not as pask_rope_init leaves it;
- * neither or both of pos_dev and first_dev; null pointers, pointers not aligned
+ * neither or both of pos_dev and first_dev; first_stride, where it is read, below
+ * 0; null pointers, pointers not aligned
  * to their elements; a stride below heads * head_dim; an output that starts at
  * its input with another stride), PASK_E_SHAPE (negative sizes, more than 1,024
  * heads, batch * max_new above 2^31 - 1), PASK_E_HIP.  With batch or max_new 0
@@ -129,8 +130,10 @@ size_t pask_prompt_workspace_bytes(const pask_geom* geom, int32_t batch, int32_t
  * to bf16 (half a step, 2^-8 of it) where the value is bf16, to fp16 (2^-11, and
  * 2^-33 of the largest) where it is LOW, and its sum is kept of the unrounded
  * ones; a LOW value is rounded once to fp16 (2^-11; 2^-20 where its page holds
- * one above 19,096, and then a key likewise).  Weights are taken relative to a reference that a score may
- * exceed by 15 in base 2 before it moves: an output element is certain to be
+ * one above 19,096, and there a key likewise); to a LOW key the queries enter
+ * as fp16, each row at a power of two that leaves its elements exact down to
+ * 2^-28 of the largest.  Weights are taken relative to a reference that a score
+ * may exceed by 15 in base 2 before it moves: an output element is certain to be
  * finite where the query's scores and the sums they are made of are finite in
  * fp32 and the magnitudes of its values, over the entries seen, sum to less than
  * 2^112.

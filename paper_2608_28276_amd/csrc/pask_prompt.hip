@@ -265,7 +265,7 @@ __device__ __forceinline__ void lds_barrier_wave() {
 // its last 3: two exact fp16, whose scores take twice the products (half as many
 // again in all); a value is rounded once (half a step, 2^-11) and meets weights
 // of fp16.  The queries become fp16 too, each row at the power of two that takes
-// its largest element below 2^15 (exact for elements down to 2^-22 of it).  Keys
+// its largest element below 2^15 (exact for elements down to 2^-28 of it).  Keys
 // of one bf16 made the outputs of int4 histories 3.4e-3 of their size wrong and
 // lse 3e-5; outputs of bf16 pages are 2.1e-3 wrong, most of it their own rounding.
 // The scores of the next 32 keys are computed beside the weights of the current
@@ -286,7 +286,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
   // last tiles of all sequences first, then the ones before them, so that the
   // tiles that end the call see the fewest keys (4 chunks of 1,123-4,096 queries
   // behind 2,258-8,192 tokens: 2,227 us with the tiles of highest number first,
-  // whichever sequence they are of, PLACE so).
+  // whichever sequence they are of, 1,677 so).
   int rest = (int)blockIdx.x;
   const int head = rest % a.cv.n_kv_heads;
   rest /= a.cv.n_kv_heads;
@@ -728,7 +728,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
 // units in two batches, one taken while the other comes.  Eight waves a compute
 // unit (two workgroups) keep up to 128 KiB on its way.  LOW pages are widened in
 // registers.  Numerics are those of prompt_kernel.
-constexpr int kFewWaves = 4, kFewRows = 32, kFewMost = 64;
+constexpr int kFewWaves = 4, kFewRows = 32;
 template <int D, int G>
 __global__ __launch_bounds__(64 * kFewWaves, 2) void prompt_few_kernel(PromptArgs a) {
   using L = PageLayout<D>;
@@ -745,14 +745,14 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void prompt_few_kernel(PromptArg
   rest /= a.cv.n_kv_heads;
   const int piece = rest % a.pieces;
   rest /= a.pieces;
-  const int b = rest % a.batch, nq = a.n_q ? min(max(a.n_q[b], 0), a.max_q) : a.max_q, n_rows = nq * G;
-  const int row0 = rest / a.batch * kFewRows, row = row0 + n;
-  if (row0 >= n_rows) return;
+  const int b = rest, nq = a.n_q ? min(max(a.n_q[b], 0), a.max_q) : a.max_q, n_rows = nq * G;
+  const int row = n;
+  if (n_rows == 0) return;
   const bool in = row < n_rows;
   const Keys keys = keys_of(a.cv, b, a.layer);
   const long long first = a.first ? (long long)a.first[b] : (long long)keys.n_pos - nq;
   // Entries of each list that the first row sees, and the last: 16 lanes for each of the four.
-  const long long wave_at = first + row0 / G, wave_end = first + (min(row0 + kFewRows, n_rows) - 1) / G;
+  const long long wave_at = first, wave_end = first + nq - 1;
   const int seen = entries_at(lane < 32 ? keys.list[0] : keys.list[1], lane < 32 ? keys.n[0] : keys.n[1], keys.n_pos,
                               lane & 16 ? wave_end : wave_at);
   const int first_sees[2] = {__builtin_amdgcn_readlane(seen, 0), __builtin_amdgcn_readlane(seen, 32)};
@@ -1063,7 +1063,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void prompt_few_kernel(PromptArg
       acc[d + 3] = fmaf(v.w, f, acc[d + 3]);
     }
   }
-  const int to = row0 + x;
+  const int to = x;
   if (to >= n_rows) return;
   if (a.pieces > 1) {
     const size_t w = (((size_t)b * a.cv.n_kv_heads + head) * a.pieces + piece) * ((size_t)a.max_q * G) + to;
@@ -1186,18 +1186,22 @@ void launch_dim(const PromptArgs& a, const PromptCut& c, hipStream_t s) {
 }  // namespace
 
 // Tiles of 256 rows, whose eight waves share every page through LDS, or of 32,
-// whose waves share the rows, where no sequence has more than kFewMost.  The keys
-// are cut into pieces where the tiles leave compute units idle.  For tiles of 256
+// whose waves share the rows, where no sequence has more (32 sequences of 1,000-
+// 8,000 tokens, 32 rows of each: 88 us so, 149 in tiles of 256; 48 rows in two
+// tiles of 32: 153, in one of 256: 155).  The keys are cut into pieces where the
+// tiles leave compute units idle: for 32 rows by the workgroups the card holds
+// (64 sequences: 1 piece 263 us bf16 / 207 int4, 2 pieces 279 / 192, 4 278 / 185;
+// one of 32,005 tokens: 32 pieces 36 us, 64 36, 128 50).  For tiles of 256
 // rows by what a call takes with each number of pieces, in microseconds: as many
 // turns of the 256 compute units as the workgroups need, each a piece's steps at
 // 2.5 (64 keys: 2.1 of bf16 pages, 3.2 of int4 ones) and 10 to begin and end, and
 // the joining, 6 and its traffic (88 tiles of 32,333 tokens, most of them int4:
-// 509 with 2 pieces, PIECES with the 8 of this rule).
+// 509 us with 2 pieces, 428 with the number of this rule).
 PromptCut prompt_cut(int32_t batch, int32_t max_q, int32_t group, int32_t n_kv_heads, int32_t head_dim,
                      int32_t max_ctx_hint) {
   PromptCut c;
   const int64_t rows = (int64_t)max_q * group;
-  c.rows = rows <= kFewMost ? kFewRows : 256;
+  c.rows = rows <= kFewRows ? kFewRows : 256;
   c.pieces = 1;
   const int64_t tiles = (rows + c.rows - 1) / c.rows * batch * n_kv_heads;
   if (c.rows == kFewRows) {                        // of 4 waves each, with a unit or more for each wave

@@ -109,7 +109,7 @@ int pask_rope_apply(const pask_rope* rope, int32_t batch, int32_t max_new, const
   if (batch < 0 || max_new < 0 || (int64_t)batch * max_new > INT32_MAX) return PASK_E_SHAPE;
   if (n_q_heads < 0 || n_k_heads < 0 || n_q_heads > PASK_ROPE_MAX_HEADS || n_k_heads > PASK_ROPE_MAX_HEADS)
     return PASK_E_SHAPE;
-  if ((pos_dev != nullptr) == (first_dev != nullptr)) return PASK_E_ARG;
+  if ((pos_dev != nullptr) == (first_dev != nullptr) || (first_dev && first_stride < 0)) return PASK_E_ARG;
   if (!aligned(pos_dev, 4) || !aligned(first_dev, 4) || !aligned(n_new_dev, 4)) return PASK_E_ARG;
   st = check_rope_rows(*rope, n_q_heads, q_in, q_in_stride, q_out, q_out_stride);
   if (st != PASK_OK) return st;

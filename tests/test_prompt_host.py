@@ -100,7 +100,7 @@ def apply_args(**kw):
     (dict(first=None), "ARG"), (dict(pos=AT), "ARG"), (dict(first=None, pos=AT + 2), "ARG"), (dict(first=AT + 1), "ARG"),
     (dict(n_new=AT + 2), "ARG"), (dict(q_in=None), "ARG"), (dict(q_out=None), "ARG"), (dict(k_in=AT + 1), "ARG"),
     (dict(k_out=AT + 1), "ARG"), (dict(q_in_stride=511), "ARG"), (dict(q_out_stride=0), "ARG"),
-    (dict(k_in_stride=-256), "ARG"), (dict(k_out_stride=1 << 41), "ARG"),
+    (dict(first_stride=-1), "ARG"), (dict(k_in_stride=-256), "ARG"), (dict(k_out_stride=1 << 41), "ARG"),
     (dict(q_out=AT, q_out_stride=520), "ARG")])
 def test_apply_refusals(bad, want):
     assert status(prompt.pask_rope_apply, **apply_args(**bad)) == getattr(pask, "PASK_E_" + want)
