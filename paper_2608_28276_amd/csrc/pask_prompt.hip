@@ -48,15 +48,15 @@ __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {   // round 
 // lds + 16 l.  In asm because the compiler waits for every copy it knows of
 // before the next read of LDS, that of another buffer too; these are waited for
 // at the workgroup's meetings alone (wait_loads).  No register is written.
-// kOnce: data read once per call (non-temporal).
+// m0 is set where it is used, as the compiler itself does.  kOnce: data read once
+// per call (non-temporal).
 template <bool kOnce>
 __device__ __forceinline__ void copy_to_lds(const uint8_t* src, uint32_t at, uint32_t lds) {
+  lds = (uint32_t)__builtin_amdgcn_readfirstlane((int)lds);
   if constexpr (kOnce)
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(at), "s"(src), "s"(lds)
-                 : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(at), "s"(src), "s"(lds) : "memory");
   else
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(at), "s"(src), "s"(lds)
-                 : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(at), "s"(src), "s"(lds) : "memory");
 }
 
 // The kinds of pages a sequence's keys come from, in the order they are taken.
@@ -299,17 +299,22 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
   const long long first = a.first ? (long long)a.first[b] : (long long)keys.n_pos - nq;
   const int row0 = tile0 + wave * 32, row = row0 + n;
   const bool in = row < n_rows;
-  // Entries of each list that the tile's last row, the wave's first and its last see, found by 16 lanes each.
+  // Entries of each list that the tile's last row sees and the wave's first, 16
+  // lanes for each of the four; and, one per lane, the positions of the next 32
+  // of both lists: the wave's rows see at most its tokens' number more.
   const long long tile_at = first + (min(tile0 + kRows, n_rows) - 1) / G, wave_at = first + row0 / G;
   const long long wave_end = first + (min(row0 + 32, n_rows) - 1) / G;
-  int n_see[2], first_sees[2], last_sees[2];
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const int seen = entries_at(keys.list[k], keys.n[k], keys.n_pos, lane < 16 ? tile_at : lane < 32 ? wave_at : wave_end);
-    n_see[k] = __builtin_amdgcn_readlane(seen, 0);
-    first_sees[k] = row0 < n_rows ? __builtin_amdgcn_readlane(seen, 16) : 0;
-    last_sees[k] = row0 < n_rows ? __builtin_amdgcn_readlane(seen, 32) : 0;
-  }
+  const int seen = entries_at(lane < 32 ? keys.list[0] : keys.list[1], lane < 32 ? keys.n[0] : keys.n[1], keys.n_pos,
+                              lane & 16 ? wave_at : tile_at);
+  const int n_see[2] = {__builtin_amdgcn_readlane(seen, 0), __builtin_amdgcn_readlane(seen, 32)};
+  const int first_of[2] = {__builtin_amdgcn_readlane(seen, 16), __builtin_amdgcn_readlane(seen, 48)};
+  const int near_at = (g ? first_of[1] : first_of[0]) + n;
+  const bool is_near = row0 < n_rows && near_at < (g ? n_see[1] : n_see[0]);
+  const int near = is_near ? (g ? keys.list[1] : keys.list[0])[near_at] : 0;
+  auto more_at = [&](long long p) { return __ballot(is_near && (long long)near <= p); };   // LOW entries below, HIGH above
+  const unsigned long long last = more_at(wave_end);
+  const int first_sees[2] = {row0 < n_rows ? first_of[0] : 0, row0 < n_rows ? first_of[1] : 0};
+  const int last_sees[2] = {first_sees[0] + (int)__popc((uint32_t)last), first_sees[1] + (int)__popc((uint32_t)(last >> 32))};
   const bool ring_seen = keys.ring_slots > 0 && tile_at >= (long long)keys.n_pos - keys.ring_slots;
   const int low_steps = (n_see[kLowPages] + kStepKeys - 1) / kStepKeys;
   const int high_steps = (n_see[kHighPages] + kStepKeys - 1) / kStepKeys;
@@ -554,19 +559,16 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
     }
   };
   int i = 2 * j_begin;
-  // The units of one kind up to u1; u0: its first.  fs, ls: entries that the wave's first and last row see.
-  auto segment = [&](auto is_low, bool ring, int u0, int u1, int fs, int ls, const int32_t* list, int used)
-      __attribute__((always_inline)) {
-    // The entries between what the wave's first and last row see are fewer than
-    // its tokens: one per lane, counted for each token.
+  // The units of one kind up to u1; u0: its first.  fs, ls: entries that the wave's first and last row see; used: of its
+  // slots.
+  auto segment = [&](auto is_low, bool ring, int u0, int u1, int fs, int ls, int used) __attribute__((always_inline)) {
     const long long at = first + (in ? row / G : 0);
-    int sees = fs;
+    int sees = fs;                                 // entries that the lane's row sees
     if (ls > fs) {
-      const int pos = lane < ls - fs ? list[fs + lane] : INT32_MAX;
 #pragma unroll 1
       for (int x = 0; x < 32 / G; ++x) {
-        const int c = __popcll(__ballot(lane < ls - fs && (long long)pos <= wave_at + x));
-        if (at == wave_at + x) sees = fs + c;
+        const unsigned long long c = more_at(wave_at + x);
+        if (at == wave_at + x) sees = fs + (int)__popc((uint32_t)(decltype(is_low)::value ? c : c >> 32));
       }
     }
     if (!in) sees = 0;
@@ -686,14 +688,14 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
   const int u_low = 2 * low_steps, u_high = 2 * (low_steps + high_steps), u_end = 2 * j_end;
   if (i < min(u_low, u_end)) {
     load_queries<true, KI>(a, q_row, in, g, qf, scale);
-    segment(std::true_type{}, false, 0, min(u_low, u_end), first_sees[0], last_sees[0], keys.list[0], keys.n[0]);
+    segment(std::true_type{}, false, 0, min(u_low, u_end), first_sees[0], last_sees[0], keys.n[0]);
   }
   if (i < u_end) load_queries<false, KI>(a, q_row, in, g, qf, scale);
 #pragma unroll 1
   for (int k = 0; k < 2; ++k) {                    // HIGH entries, then the window's
     const int to = k ? u_end : min(u_high, u_end);
     if (i >= to) continue;
-    segment(std::false_type{}, k == 1, k ? u_high : u_low, to, k ? 0 : first_sees[1], k ? 0 : last_sees[1], keys.list[1],
+    segment(std::false_type{}, k == 1, k ? u_high : u_low, to, k ? 0 : first_sees[1], k ? 0 : last_sees[1],
             k ? keys.ring_slots : keys.n[1]);
   }
   wait_loads();                                    // copies that repeat the last step: none is left behind
@@ -1118,13 +1120,20 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(PromptArgs a) {
 #pragma unroll
       for (int d = 0; d < E; ++d) o[d] *= keep;
       top = ref;
-#pragma unroll 8
-      for (int p = 0; p < n; ++p) {
-        const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), p));
-        if (f == 0.0f) continue;
-        const float* from = a.ws_o + (first + (size_t)(p0 + p * kWaves) * rows) * D + lane * E;
+      for (int p = 0; p < n; p += 8) {             // 8 at a time: their loads together, those behind the last one its own
+        float f[8], v[8][E];
 #pragma unroll
-        for (int d = 0; d < E; ++d) o[d] = fmaf(from[d], f, o[d]);
+        for (int y = 0; y < 8; ++y) {
+          const int at = min(p + y, n - 1);
+          f[y] = p + y < n ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), at)) : 0.0f;
+          const float* from = a.ws_o + (first + (size_t)(p0 + at * kWaves) * rows) * D + lane * E;
+#pragma unroll
+          for (int d = 0; d < E; ++d) v[y][d] = from[d];
+        }
+#pragma unroll
+        for (int y = 0; y < 8; ++y)
+#pragma unroll
+          for (int d = 0; d < E; ++d) o[d] = f[y] == 0.0f ? o[d] : fmaf(v[y][d], f[y], o[d]);
       }
     }
   }

@@ -173,3 +173,21 @@ def test_workspace_bytes():
     assert ws(g, 1, 4, 0) == ws(g, 1, 4, 1 << 18) == ws(g, 1, 4, (1 << 18) + 5)
     assert ws(g, 0, 4, 0) == ws(g, 65, 4, 0) == ws(g, 1, 0, 0) == ws(g, 1, -1, 0) == 0
     assert ws(geom(head_dim=96), 1, 4, 0) == 0
+
+
+def test_workspace_of_any_call_is_bounded_and_asked_for():
+    """At most 1,024 workgroups of 256 rows leave partial results; one byte less is refused."""
+    import random
+    rng = random.Random(5)
+    for _ in range(400):
+        group, kv, d = rng.choice([1, 2, 4, 8]), rng.randint(1, 8), rng.choice([64, 128])
+        g = geom(max_batch=rng.randint(1, 300), n_q_heads=group * kv, n_kv_heads=kv, head_dim=d,
+                 max_tokens_per_seq=1 << rng.randint(4, 17), recent_window=rng.choice([0, 5]))
+        batch = rng.randint(1, g.max_batch)
+        max_q = max(1, int(g.max_tokens_per_seq * rng.random() ** 4))
+        need = prompt.pask_prompt_workspace_bytes(g, batch, max_q, 0)
+        assert need <= 2048 * 256 * (d + 2) * 4 + 1024
+        if need:
+            assert need % 256 == 0
+            args = attn_args(cache=fake_cache(g), batch=batch, max_q=max_q, ws_bytes=need - 1)
+            assert status(prompt.pask_prompt_attn, **args) == pask.PASK_E_CAPACITY
