@@ -3,6 +3,7 @@
 // into pieces where there are few queries.
 #include <hip/hip_runtime.h>
 
+#include <float.h>
 #include <math.h>
 
 #include <algorithm>
@@ -185,7 +186,7 @@ __device__ __forceinline__ void load_queries(const PromptArgs& a, size_t q_row, 
     if (kLow) most = max(most, abs_max_bits8(qf[i]));
     qf[i] = make_uint4(qf[i].x ^ flip, qf[i].y ^ flip, qf[i].z ^ flip, qf[i].w ^ flip);
   }
-  scale = fabsf(a.scale_log2);
+  scale = fmaxf(fabsf(a.scale_log2), FLT_MIN);     // above 0, so that a hidden score of -inf stays that
   if constexpr (kLow) {
     most = max(most, (uint32_t)__shfl_xor((int)most, 32));
     const int up = 14 - ((int)(most >> 7) - 127);
@@ -196,7 +197,7 @@ __device__ __forceinline__ void load_queries(const PromptArgs& a, size_t q_row, 
       qf[i] = make_uint4(two(bf16_lo(q.x), bf16_lo(q.y)), two(bf16_hi(q.x), bf16_hi(q.y)),
                          two(bf16_lo(q.z), bf16_lo(q.w)), two(bf16_hi(q.z), bf16_hi(q.w)));
     }
-    scale = ldexpf(scale, -up);
+    scale = fmaxf(ldexpf(scale, -up), FLT_MIN);
   }
 }
 // Weights of a page's 16 slots as an operand; for LOW values in code_pair's order.
@@ -610,13 +611,11 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
       // One unit by itself, as at the edge: some row of the wave does not see all its keys.
       const int slot0 = 32 * (i - u0);
       if (row0 < n_rows && (ring || ls > slot0)) {
-        uint32_t hidden = 0u;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
+        const bool edge = ring || fs < slot0 + 32;
+        auto hides = [&](int r) {                  // the lane's row, the unit's slot of score r
           const int k = slot0 + 8 * (r >> 2) + 4 * g + (r & 3);
-          const bool hid = ring ? !in || ring_position(keys, a.cv.window, k) > at : k >= sees;
-          hidden |= (uint32_t)hid << r;
-        }
+          return ring ? !in || ring_position(keys, a.cv.window, k) > at : k >= sees;
+        };
         s = scores(is_low, i);
         if constexpr (decltype(is_low)::value)
 #pragma unroll
@@ -624,14 +623,15 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
             if (s_wide[slot][4 * (i & 1) + 2 * h])
 #pragma unroll
               for (int r = 0; r < 8; ++r) s[8 * h + r] *= kWide;
+        if (edge)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = hidden >> r & 1u ? -INFINITY : s[r];
-        refer(highest(s));
+          for (int r = 0; r < 16; ++r) s[r] = hides(r) ? -INFINITY : s[r];
+        top = highest(s);
+        if (exceeds(top)) refer(top);
         base = mx == -INFINITY ? 0.0f : mx;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const float w = __builtin_amdgcn_exp2f(fmaf(s[r], scale, -base));
-          s[r] = hidden >> r & 1u ? 0.0f : w;
+        for (int r = 0; r < 16; ++r) {             // 0 for what is hidden
+          s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale, -base));
           sum += s[r];
         }
         const uint32_t vs = fresh(unit_at(slot, i) + v_at), vs2 = fresh(vs + 512);
@@ -639,37 +639,49 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             const uint4 p = packed_weights<decltype(is_low)::value>(s, h);
-            const float unit = s_wide[slot][4 * (i & 1) + 2 * h + 1] ? kWide : 1.0f;
+            const bool wide = __builtin_amdgcn_readfirstlane((int)s_wide[slot][4 * (i & 1) + 2 * h + 1]) != 0;
+            if (wide)
 #pragma unroll
-            for (int m = 0; m < VT; ++m) {
-              o[m] *= 1.0f / unit;
-              o[m] = add_product(is_low, value_operand(vs, vs2, h, m), p, o[m]);
-              o[m] *= unit;
-              __builtin_amdgcn_sched_barrier(0);
-            }
+              for (int m = 0; m < VT; ++m) o[m] *= 1.0f / kWide;
+#pragma unroll
+            for (int m = 0; m < VT; ++m) o[m] = add_product(is_low, value_operand(vs, vs2, h, m), p, o[m]);
+            if (wide)
+#pragma unroll
+              for (int m = 0; m < VT; ++m) o[m] *= kWide;
           }
         } else {
           // Slots behind the last entry hold what was there before: taken as 0.
           const int valid = used - slot0;
-          auto both = [&](int t) { return (t < valid ? 0xFFFFu : 0u) | (t + 1 < valid ? 0xFFFF0000u : 0u); };
+          uint4 mask[2] = {make_uint4(~0u, ~0u, ~0u, ~0u), make_uint4(~0u, ~0u, ~0u, ~0u)};
+          if (valid < 32) {
+            auto both = [&](int t) { return (t < valid ? 0xFFFFu : 0u) | (t + 1 < valid ? 0xFFFF0000u : 0u); };
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const int t = 16 * h + 4 * g;
+              mask[h] = make_uint4(both(t), both(t + 2), both(t + 8), both(t + 10));
+            }
+          }
           auto operand = [&](int h, int m) {
             const uint4 x = value_operand(vs, vs2, h, m);
-            const int t = 16 * h + 4 * g;
-            return make_uint4(x.x & both(t), x.y & both(t + 2), x.z & both(t + 8), x.w & both(t + 10));
+            return make_uint4(x.x & mask[h].x, x.y & mask[h].y, x.z & mask[h].z, x.w & mask[h].w);
           };
           bool wild = false;                       // some value is infinite or NaN
+          if (edge)
 #pragma unroll
-          for (int h = 0; h < 2; ++h)
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int m = 0; m < VT; ++m) wild |= abs_max_bits8(operand(h, m)) >= 0x7F80u;
+              for (int m = 0; m < VT; ++m) wild |= abs_max_bits8(operand(h, m)) >= 0x7F80u;
           __builtin_amdgcn_sched_barrier(0);
           if (__ballot(wild)) {
             const uint8_t* v0 = s_kv[slot] + (i & 1) * 2 * kTile + kValues;
+            uint32_t hidden = 0u;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) hidden |= (uint32_t)hides(r) << r;
             add_seen_values<VT>(v0, v0 + kTile, s, hidden, o, g, n);
           } else {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              const uint4 p = packed_weights<decltype(is_low)::value>(s, h);
+              const uint4 p = packed_weights<false>(s, h);
 #pragma unroll
               for (int m = 0; m < VT; ++m) o[m] = mfma(operand(h, m), p, o[m]);
             }
