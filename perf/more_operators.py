@@ -288,8 +288,9 @@ def _session(case):
     lens = [a + b for a, b in zip(_news(case), _pasts(case))]
     pages = sum((n + 15) // 16 for n in lens)
     return PaskSession(_blob(case), max_batch=case["batch"], n_layers=1, n_q_heads=case["q_heads"],
-                       n_kv_heads=case["kv_heads"], head_dim=case["head_dim"], max_tokens_per_seq=max(lens),
-                       hi_pages=pages, lo_pages=pages if case["lo"] else 0)
+                       n_kv_heads=case["kv_heads"], head_dim=case["head_dim"],
+                       max_tokens_per_seq=max(lens + [case["window"]]), hi_pages=pages,
+                       lo_pages=pages if case["lo"] else 0)
 
 
 def prepare(case, seed):
