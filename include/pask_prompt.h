@@ -105,7 +105,7 @@ int pask_rope_apply(const pask_rope* rope, int32_t batch, int32_t max_new, const
  * most persisted entries of a sequence, window included; a larger count is
  * still correct, only less parallel; below 1 or above max_tokens_per_seq it
  * counts as max_tokens_per_seq).  0 where it needs none, and for an invalid
- * geometry, batch outside 1..max_batch or max_q below 0. */
+ * geometry, batch outside 1..max_batch or max_q outside 1..max_tokens_per_seq. */
 size_t pask_prompt_workspace_bytes(const pask_geom* geom, int32_t batch, int32_t max_q, int32_t max_ctx_hint);
 
 /* Attention of many query tokens of each sequence over the persisted history
