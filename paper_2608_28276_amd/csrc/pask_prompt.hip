@@ -1224,11 +1224,12 @@ void launch_dim(const PromptArgs& a, const PromptCut& c, hipStream_t s) {
 
 // Tiles of 256 rows, whose eight waves share every page through LDS, or of 32,
 // whose waves share the rows, where no sequence has more (32 sequences of 1,000-
-// 8,000 tokens, 32 rows of each: 88 us so, 149 in tiles of 256; 48 rows in two
-// tiles of 32: 153, in one of 256: 155).  The keys are cut into pieces where the
-// tiles leave compute units idle: for 32 rows by the workgroups the card holds
-// (64 sequences: 1 piece 263 us bf16 / 207 int4, 2 pieces 279 / 192, 4 278 / 185;
-// one of 32,005 tokens: 32 pieces 36 us, 64 36, 128 50).  For tiles of 256
+// 8,000 tokens, 32 rows of each: 82 us so, 150 in tiles of 256; 48 rows, in a build
+// before, in two tiles of 32: 153, in one of 256: 155).  The keys are cut into
+// pieces where the tiles leave compute units idle: for 32 rows by the workgroups the
+// card holds (8 KV heads; with 1, 2 and 4 pieces 128 sequences of 500-4,096 tokens
+// take 134, 147, 159 us, 64 of 1,024-8,192 124, 124, 140, 32 of 1,000-8,000 97, 82,
+// 81; one of 32,005 tokens with 32, 64 and 128 pieces 31, 29, 43).  For tiles of 256
 // rows by what a call takes with each number of pieces, in microseconds: as many
 // turns of the 256 compute units as the workgroups need, each a piece's steps at
 // 2.5 (64 keys: 2.1 of bf16 pages, 3.2 of int4 ones) and 10 to begin and end, and
