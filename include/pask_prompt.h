@@ -129,10 +129,9 @@ size_t pask_prompt_workspace_bytes(const pask_geom* geom, int32_t batch, int32_t
  * score exactly; a softmax weight is rounded once for its product with the value,
  * to bf16 (half a step, 2^-8 of it) where the value is bf16, to fp16 (2^-11, and
  * 2^-33 of the largest) where it is LOW, and its sum is kept of the unrounded
- * ones; a LOW value is rounded once to fp16 (2^-11; 2^-20 where its page holds
- * one above 19,096, and there a key likewise); to a LOW key the queries enter
- * as fp16, each row at a power of two that leaves its elements exact down to
- * 2^-28 of the largest.  Weights are taken relative to a reference that a score
+ * ones; a LOW value is rounded once to fp16 (2^-11 of it, whatever else its page
+ * holds); to a LOW key the queries enter as fp16, each row at a power of two
+ * that leaves its elements exact down to 2^-28 of the largest.  Weights are taken relative to a reference that a score
  * may exceed by 15 in base 2 before it moves: an output element is certain to be
  * finite where the query's scores and the sums they are made of are finite in
  * fp32 and the magnitudes of its values, over the entries seen, sum to less than

@@ -150,10 +150,27 @@ struct LowPart {
   uint32_t code[NG];
   uint32_t scale[2 * NG];                          // keys: the first NG / 2
 };
-// A page with a scale above this (fp16 bits of 2728) is taken at 1 / 32 of its
-// elements: 24 scales, and 7, are below the largest fp16.
+// A scale above this (fp16 bits of 2728) is wide: it is taken at 1 / 32, which
+// is exact there, so that 24 scales, and 7, are below the largest fp16.  The
+// other scales stay as they are (at 1 / 32 the small ones would lose bits), so
+// wide groups have products of their own, between a factor of 1 / 32 and one of
+// 32 on the sums.  That is slow, and rare: 8,192 queries over as many int4 tokens,
+// every scale wide, take 3,580 us where others take 827, 64 drafts 645 and 137.
 constexpr uint32_t kWideScale = 0x6954u;
 constexpr float kWide = 32.0f;
+// Of a word's two scales those that are wide, as a mask.
+__device__ __forceinline__ uint32_t wide_mask(uint32_t scales) {
+  return ((uint32_t)((int)(kWideScale - (scales & 0xFFFFu)) >> 31) & 0xFFFFu) |
+         ((uint32_t)((int)(kWideScale - (scales >> 16)) >> 31) << 16);
+}
+__device__ __forceinline__ uint32_t at_1_32(uint32_t scales) {
+  return word_of(halves(scales) * (f16x2_t){(_Float16)(1.0f / kWide), (_Float16)(1.0f / kWide)});
+}
+// The scales that one of a wide page's two products takes: the wide ones' or the others', 0 for the rest.
+__device__ __forceinline__ uint32_t scales_of(bool wide, uint32_t scales) {
+  const uint32_t m = wide_mask(scales);
+  return wide ? at_1_32(scales) & m : scales & ~m;
+}
 
 // O += P V key by key over 32 keys (values of pages at v0 and v1), where a value
 // that some query does not see is infinite or NaN (a weight of 0 times it is
@@ -296,7 +313,8 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
   // A page in LDS: keys, the rest of LOW keys, values.
   constexpr int kPart = L::kHiV, kValues = 2 * kPart, kTile = 3 * kPart, kStep = kStepPages * kTile;
   __shared__ __align__(1024) uint8_t s_kv[3][kStep];
-  __shared__ __align__(16) uint32_t s_wide[3][2 * kStepPages];   // LOW parts (keys, values of a page) at 1 / 32
+  // LOW parts (keys, values of a page) with a wide scale; of those, which slots' scale is, for each group.
+  __shared__ __align__(16) uint32_t s_wide[3][2 * kStepPages], s_wide_slots[3][2 * kStepPages][NG];
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int g = lane >> 5, n = lane & 31;
   // Workgroups go to the 8 XCDs in turn: neighbours are different KV heads.  The
@@ -424,9 +442,27 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
       for (int c = 1; c < 2 * NG; ++c)
         if (c < NG / 2 || values) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2_t, sc[c]));
       const bool wide = __ballot(max(most[0], most[1]) > kWideScale) != 0ull;
-      if (wide) {
+      if (__builtin_expect(wide, 0)) {
 #pragma unroll
-        for (int c = 0; c < 2 * NG; ++c) sc[c] = word_of(halves(sc[c]) * (f16x2_t){(_Float16)(1.0f / kWide), (_Float16)(1.0f / kWide)});
+        for (int i = 0; i < NG; ++i) {
+          uint32_t of = 0u;                        // of the lane's slots those wide in group i, one bit each
+#pragma unroll
+          for (int t = 0; t < 4; ++t)
+            if (t == 0 || values) of |= wide_mask(sc[t * (NG / 2) + i / 2]) >> (16 * (i & 1)) & 1u << t;
+          if (values) {                            // lane 16 y's slots 4 y ..
+            of <<= lane >> 4 << 2;
+            of |= (uint32_t)__shfl_xor((int)of, 16);
+            of |= (uint32_t)__shfl_xor((int)of, 32);
+          } else {                                 // lane t's slot t
+            of = (uint32_t)__ballot(of != 0u) & 0xFFFFu;
+          }
+          if (lane == 0) s_wide_slots[j % 3][x][i] = of;
+        }
+#pragma unroll
+        for (int c = 0; c < 2 * NG; ++c) {
+          const uint32_t m = wide_mask(sc[c]);
+          sc[c] = (at_1_32(sc[c]) & m) | (sc[c] & ~m);
+        }
       }
       if (lane == 0) s_wide[j % 3][x] = wide;
       const uint32_t at = dst + p * kTile + (values ? kValues : 0) + lane * 16;
@@ -496,6 +532,27 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
       s = add_product(is_low, ring[k % kAhead], query_operand(is_low, k), s);
       if (k + kAhead < kProducts) ring[k % kAhead] = key_operand(is_low, ks, k + kAhead);
       __builtin_amdgcn_sched_barrier(0);
+    }
+    return s;
+  };
+  // The same of LOW keys with wide groups: the other groups' products, then theirs at 1 / 32.
+  auto wide_scores = [&](int i) __attribute__((always_inline)) {
+    f32x16_t s;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = 0.0f;
+#pragma unroll 1
+    for (int wide = 0; wide < 2; ++wide) {
+      const int l = fresh(lane), part = 8 * slot + 4 * (i & 1) + 2 * (l >> 4 & 1);   // the keys of the page of the lane's slot
+      const uint32_t ks = fresh(unit_at(slot, i) + k_at), some = (&s_wide[0][0])[part] ? 1u << (l & 15) : 0u;
+      const uint32_t* slots_of = s_wide_slots[0][part];
+#pragma unroll
+      for (int k = 0; k < 2 * KI; ++k) {
+        const uint32_t take = ((slots_of[k / 4] & some) != 0u) == (wide != 0) ? ~0u : 0u;
+        const uint4 x = key_operand(std::true_type{}, ks, k);
+        s = mfma_half(make_uint4(x.x & take, x.y & take, x.z & take, x.w & take), qf[k >> 1], s);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      s *= wide ? kWide : 1.0f / kWide;
     }
     return s;
   };
@@ -632,13 +689,10 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
           const int k = slot0 + 8 * (r >> 2) + 4 * g + (r & 3);
           return ring ? !in || ring_position(keys, a.cv.window, k) > at : k >= sees;
         };
-        s = scores(is_low, i);
-        if constexpr (decltype(is_low)::value)
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-            if (s_wide[slot][4 * (i & 1) + 2 * h])
-#pragma unroll
-              for (int r = 0; r < 8; ++r) s[8 * h + r] *= kWide;
+        const uint32_t* wide_parts = &s_wide[slot][4 * (i & 1)];   // keys, values of the unit's two pages
+        const bool wide_keys = decltype(is_low)::value && __builtin_amdgcn_readfirstlane((int)(wide_parts[0] | wide_parts[2]));
+        if (__builtin_expect(wide_keys, 0)) s = wide_scores(i);
+        else s = scores(is_low, i);
         if (edge)
 #pragma unroll
           for (int r = 0; r < 16; ++r) s[r] = hides(r) ? -INFINITY : s[r];
@@ -655,15 +709,26 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             const uint4 p = packed_weights<decltype(is_low)::value>(s, h);
-            const bool wide = __builtin_amdgcn_readfirstlane((int)s_wide[slot][4 * (i & 1) + 2 * h + 1]) != 0;
-            if (wide)
+            if (!__builtin_amdgcn_readfirstlane((int)wide_parts[2 * h + 1])) {
 #pragma unroll
-              for (int m = 0; m < VT; ++m) o[m] *= 1.0f / kWide;
+              for (int m = 0; m < VT; ++m) o[m] = add_product(is_low, value_operand(vs, vs2, h, m), p, o[m]);
+              continue;
+            }
+#pragma unroll 1
+            for (int wide = 0; wide < 2; ++wide) {
+              const uint32_t at0 = fresh(vs), at1 = fresh(vs + 512);
+              const uint32_t* slots_of = s_wide_slots[0][fresh(8 * slot + 4 * (i & 1) + 2 * h + 1)];
+              const int t = fresh(4 * g);
 #pragma unroll
-            for (int m = 0; m < VT; ++m) o[m] = add_product(is_low, value_operand(vs, vs2, h, m), p, o[m]);
-            if (wide)
-#pragma unroll
-              for (int m = 0; m < VT; ++m) o[m] *= kWide;
+              for (int m = 0; m < VT; ++m) {       // dimensions of group m: the weights of the slots that are wide there, or not
+                const uint32_t of = (slots_of[m] ^ (wide ? 0u : ~0u)) >> t;
+                auto both = [&](int x) { return (of >> x & 1u ? 0xFFFFu : 0u) | (of >> (x + 2) & 1u ? 0xFFFF0000u : 0u); };
+                const uint4 q = make_uint4(p.x & both(0), p.y & both(1), p.z & both(8), p.w & both(9));
+                o[m] = add_product(is_low, value_operand(at0, at1, h, m), q, o[m]);
+                o[m] *= wide ? kWide : 1.0f / kWide;
+                __builtin_amdgcn_sched_barrier(0);
+              }
+            }
           }
         } else {
           // Slots behind the last entry hold what was there before: taken as 0.
@@ -776,9 +841,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void prompt_few_kernel(PromptArg
   const int piece = rest % a.pieces;
   rest /= a.pieces;
   const int b = by_length(a, rest), nq = a.n_q ? min(max(a.n_q[b], 0), a.max_q) : a.max_q, n_rows = nq * G;
-  const int row = n;
   if (n_rows == 0) return;
-  const bool in = row < n_rows;
+  const bool in = n < n_rows;
   const Keys keys = keys_of(a.cv, b, a.layer);
   const long long first = a.first ? (long long)a.first[b] : (long long)keys.n_pos - nq;
   // Entries of each list that the first row sees, and the last: 16 lanes for each of the four.
@@ -792,7 +856,12 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void prompt_few_kernel(PromptArg
   const int units = u_high + (ring_seen ? (keys.ring_slots + 31) / 32 : 0);
   const int part = piece * kFewWaves + wave, parts = a.pieces * kFewWaves;
   const int begin = (int)((long long)units * part / parts), end = (int)((long long)units * (part + 1) / parts);
-  const size_t q_row = (((size_t)b * a.max_q + (in ? row / G : 0)) * a.n_q_heads + (size_t)head * G + (in ? row % G : 0));
+  // The lane's row of the queries, and its position: made where they are used, which is rarely.
+  auto q_row = [&] {
+    const int x = fresh(in ? n : 0);
+    return ((size_t)b * a.max_q + x / G) * a.n_q_heads + (size_t)head * G + x % G;
+  };
+  auto row_at = [&] { return first + fresh(in ? n : 0) / G; };
 
   // Where the head's part of the pages starts, 64 pages at a time, one per lane.
   auto kind_of = [&](int u) { return u < u_low ? kLowPages : u < u_high ? kHighPages : kWindowPages; };
@@ -826,7 +895,6 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void prompt_few_kernel(PromptArg
     for (int r = 0; r < 16; ++r) o[m][r] = 0.0f;
   float mx = -INFINITY, sum = 0.0f;
   const uint32_t room = lds_address(s_room[wave]);
-  const long long at = first + (in ? row / G : 0);
   const int t16 = n & 15, own = n >> 4;            // slot of a page, and which of a unit's two; of values: dimension, parity
   int u = begin;
   // The wave's units of one kind up to `to`; u0: the kind's first.
@@ -857,11 +925,12 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void prompt_few_kernel(PromptArg
       copy_half(u, 0);
       copy_half(u, 1);
     }
-    load_queries<kLow, KI>(a, q_row, in, g, qf, scale);
+    load_queries<kLow, KI>(a, q_row(), in, g, qf, scale);
     // What each row sees: the entries between what the first and the last row see are fewer than the tile's tokens.
     int sees = fs;
     if (ls > fs) {
       const int pos = lane < ls - fs ? list[fs + lane] : INT32_MAX;
+      const long long at = row_at();
 #pragma unroll 1
       for (int x = 0; x < kFewRows / G; ++x) {
         const int c = __popcll(__ballot(lane < ls - fs && (long long)pos <= wave_at + x));
@@ -888,8 +957,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void prompt_few_kernel(PromptArg
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] = 0.0f;
         const int valid = used - slot0;            // of the unit's slots; what was there before is behind them
-        bool wide_keys = false, wide_values = false;   // of a unit with a wide page: taken at 1 / 32
-        const f16x2_t down = {(_Float16)(1.0f / kWide), (_Float16)(1.0f / kWide)};
+        bool wide_keys = false, wide_values = false;   // some of the unit's scales are
         const uint32_t low0 = room + slot * (kRoom / 2) + 2 * x * L::kLoHead;
         if constexpr (kLow) {
           // A page's scales are 8 NG words, NG / 2 a slot.
@@ -907,24 +975,37 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void prompt_few_kernel(PromptArg
           read_words(k0 + L::kLoKS + t16 * 2 * NG, ks);
           read_words(k0 + (g * 16 + t16) * 4 * NG, word0);
           read_words(k0 + ((g + 2) * 16 + t16) * 4 * NG, word1);
-          if (16 * own + t16 >= valid)
-#pragma unroll
-            for (int c = 0; c < NG / 2; ++c) ks[c] = 0u;
-          if (wide_keys)
-#pragma unroll
-            for (int c = 0; c < NG / 2; ++c) ks[c] = word_of(halves(ks[c]) * down);
-#pragma unroll
-          for (int i = 0; i < NG; ++i) {
-            const uint32_t both = __builtin_amdgcn_perm(ks[i / 2], ks[i / 2], i & 1 ? 0x03020302u : 0x01000100u);
+          auto add_keys = [&](int i, uint32_t scales, uint32_t w0, uint32_t w1) __attribute__((always_inline)) {   // group i
+            const uint32_t both = __builtin_amdgcn_perm(scales, scales, i & 1 ? 0x03020302u : 0x01000100u);
             const f16x2_t s8 = halves(both & 0xFFF8FFF8u), s3 = halves(both) - s8;
 #pragma unroll
             for (int w = 0; w < 2; ++w) {          // quarters g and g + 2: chunks 2 (2 i + w) + g
-              const uint32_t word = w ? word1[i] : word0[i];
+              const uint32_t word = w ? w1 : w0;
               s = mfma_half(key_part(word, s8), qf[2 * i + w], s);
               s = mfma_half(key_part(word, s3), qf[2 * i + w], s);
             }
+          };
+          if (!wide_keys) {
+            if (16 * own + t16 >= valid)
+#pragma unroll
+              for (int c = 0; c < NG / 2; ++c) ks[c] = 0u;
+#pragma unroll
+            for (int i = 0; i < NG; ++i) add_keys(i, ks[i / 2], word0[i], word1[i]);
+          } else {
+#pragma unroll 1
+            for (int wide = 0; wide < 2; ++wide) { // the groups that are not wide, then those that are
+              const int l = fresh(lane), t = l & 15;
+              const uint32_t at = low0 + (l >> 4 & 1) * L::kLoHead;
+#pragma unroll
+              for (int i = 0; i < NG; ++i) {
+                const uint32_t scales = (l & 31) < valid ? scales_of(wide != 0, read_lds4(at + L::kLoKS + t * 2 * NG + 4 * (i / 2))) : 0u;
+                const uint32_t word = at + ((l >> 5) * 16 + t) * 4 * NG + 4 * i;
+                add_keys(i, scales, read_lds4(word), read_lds4(word + 128 * NG));
+                __builtin_amdgcn_sched_barrier(0);
+              }
+              s *= wide ? kWide : 1.0f / kWide;
+            }
           }
-          if (wide_keys) s *= kWide;
         } else {
           const uint32_t k0 = fresh(room + own * kPart + g * 256 + t16 * 16);
 #pragma unroll
@@ -942,6 +1023,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void prompt_few_kernel(PromptArg
         const bool edge = ring || fs < slot0 + 32;
         uint32_t hidden = 0u;
         if (edge) {
+          const long long at = row_at();
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
             const int k = slot0 + 8 * (r >> 2) + 4 * g + (r & 3);
@@ -977,40 +1059,60 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void prompt_few_kernel(PromptArg
           }
         }
         if constexpr (kLow) {
-          if (wide_values)
+          if (!wide_values) {
 #pragma unroll
-            for (int m = 0; m < VT; ++m) o[m] *= 1.0f / kWide;
+            for (int h = 0; h < 2; ++h) {
+              uint32_t v[VT][4];
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            uint32_t v[VT][4];
+              for (int w = 0; w < 2; ++w) {        // slots 4 g .. and 4 g + 8 .., the parity's nibbles
+                uint32_t vs[2 * NG], code[NG];
+                read_words(low0 + h * L::kLoHead + L::kLoVS + (g + 2 * w) * 8 * NG, vs);
+                read_words(low0 + h * L::kLoHead + L::kLoVC + ((g + 2 * w) * 16 + t16) * 4 * NG, code);
+                if (valid < 32)
 #pragma unroll
-            for (int w = 0; w < 2; ++w) {          // slots 4 g .. and 4 g + 8 .., the parity's nibbles
-              uint32_t vs[2 * NG], code[NG];
-              read_words(low0 + h * L::kLoHead + L::kLoVS + (g + 2 * w) * 8 * NG, vs);
-              read_words(low0 + h * L::kLoHead + L::kLoVC + ((g + 2 * w) * 16 + t16) * 4 * NG, code);
-              if (valid < 32)
+                  for (int c = 0; c < 2 * NG; ++c)
+                    if (16 * h + 4 * (g + 2 * w) + c / (NG / 2) >= valid) vs[c] = 0u;
 #pragma unroll
-                for (int c = 0; c < 2 * NG; ++c)
-                  if (16 * h + 4 * (g + 2 * w) + c / (NG / 2) >= valid) vs[c] = 0u;
-              if (wide_values)
+                for (int m = 0; m < VT; ++m) {
+                  const uint32_t pick = m & 1 ? 0x07060302u : 0x05040100u;
 #pragma unroll
-                for (int c = 0; c < 2 * NG; ++c) vs[c] = word_of(halves(vs[c]) * down);
+                  for (int t = 0; t < 2; ++t)
+                    v[m][2 * w + t] = word_of(code_pair(code[m] >> (4 * own), t) *
+                                              halves(__builtin_amdgcn_perm(vs[(t + 2) * (NG / 2) + m / 2], vs[t * (NG / 2) + m / 2], pick)));
+                }
+              }
+              const uint4 p = packed_weights<true>(s, h);
+#pragma unroll
+              for (int m = 0; m < VT; ++m) o[m] = mfma_half(make_uint4(v[m][0], v[m][1], v[m][2], v[m][3]), p, o[m]);
+            }
+          } else {
+            const uint4 p0 = packed_weights<true>(s, 0), p1 = packed_weights<true>(s, 1);
+#pragma unroll 1
+            for (int x = 0; x < 4; ++x) {          // both pages' groups that are not wide, then those that are
+              const int h = x & 1, l = fresh(lane), slot_at = 16 * h + 4 * (l >> 5);
+              const bool wide = x >= 2;
+              const uint4 p = make_uint4(h ? p1.x : p0.x, h ? p1.y : p0.y, h ? p1.z : p0.z, h ? p1.w : p0.w);
+              const uint32_t scales = low0 + h * L::kLoHead + L::kLoVS + (l >> 5) * 8 * NG;
+              const uint32_t codes = low0 + h * L::kLoHead + L::kLoVC + ((l >> 5) * 16 + (l & 15)) * 4 * NG;
 #pragma unroll
               for (int m = 0; m < VT; ++m) {
-                const uint32_t pick = m & 1 ? 0x07060302u : 0x05040100u;
+                uint32_t v[4];
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
-                  v[m][2 * w + t] = word_of(code_pair(code[m] >> (4 * own), t) *
-                                            halves(__builtin_amdgcn_perm(vs[(t + 2) * (NG / 2) + m / 2], vs[t * (NG / 2) + m / 2], pick)));
+                for (int y = 0; y < 4; ++y) {      // slots t and t + 2
+                  const int w = y >> 1, t = y & 1;
+                  auto scale_at = [&](int z) {
+                    return slot_at + 8 * w + z < valid ? scales_of(wide, read_lds4(scales + 16 * w * NG + z * 2 * NG + 4 * (m / 2))) : 0u;
+                  };
+                  const uint32_t code = read_lds4(codes + w * 128 * NG + 4 * m);
+                  v[y] = word_of(code_pair(code >> (l >> 2 & 4), t) *
+                                 halves(__builtin_amdgcn_perm(scale_at(t + 2), scale_at(t), m & 1 ? 0x07060302u : 0x05040100u)));
+                }
+                o[m] = mfma_half(make_uint4(v[0], v[1], v[2], v[3]), p, o[m]);
+                if (h) o[m] *= wide ? kWide : 1.0f / kWide;
+                __builtin_amdgcn_sched_barrier(0);
               }
             }
-            const uint4 p = packed_weights<true>(s, h);
-#pragma unroll
-            for (int m = 0; m < VT; ++m) o[m] = mfma_half(make_uint4(v[m][0], v[m][1], v[m][2], v[m][3]), p, o[m]);
           }
-          if (wide_values)
-#pragma unroll
-            for (int m = 0; m < VT; ++m) o[m] *= kWide;
         } else {
           if (next < to) wait_copies<kHalf>();
           else wait_copies<0>();
