@@ -572,6 +572,8 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
     for (int m = 0; m < VT; ++m) o[m] *= alpha;
     mx = ref;
   };
+  // The weights' base: 0 while every score was -Inf (their weights are 0, and -Inf - -Inf is not).
+  auto base_of_weights = [&] { return mx == -INFINITY ? 0.0f : mx; };
   auto any_wide = [&](int s) {
     const uint4 x = *reinterpret_cast<const uint4*>(s_wide[s]), y = *reinterpret_cast<const uint4*>(s_wide[s] + 4);
     return __builtin_amdgcn_readfirstlane((int)(x.x | x.y | x.z | x.w | y.x | y.y | y.z | y.w)) != 0;
@@ -654,13 +656,13 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
         f32x16_t t;
         s = scores(is_low, i);
         refer(highest(s));
-        base = mx;
+        base = base_of_weights();
         auto follow = [&] {                        // rarely: the reference behind the next scores' maximum
           if (!exceeds(top)) return;
           sum += odd_sum;
           odd_sum = 0.0f;
           refer(top);
-          base = mx;
+          base = base_of_weights();
         };
         bool more;
         do {                                       // (one way out: a second one costs copies of the sums)
@@ -698,7 +700,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
           for (int r = 0; r < 16; ++r) s[r] = hides(r) ? -INFINITY : s[r];
         top = highest(s);
         if (exceeds(top)) refer(top);
-        base = mx == -INFINITY ? 0.0f : mx;
+        base = base_of_weights();
 #pragma unroll
         for (int r = 0; r < 16; ++r) {             // 0 for what is hidden
           s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale, -base));
