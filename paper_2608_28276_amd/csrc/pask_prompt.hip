@@ -45,21 +45,6 @@ __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {   // round 
   return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t){lo, hi}, f16x2_t));
 }
 
-// 16 bytes per lane from src (the same for the wave) + at into LDS: lane l's to
-// lds + 16 l.  In asm because the compiler waits for every copy it knows of
-// before the next read of LDS, that of another buffer too; these are waited for
-// at the workgroup's meetings alone (wait_loads).  No register is written.
-// m0 is set where it is used, as the compiler itself does.  kOnce: data read once
-// per call (non-temporal).
-template <bool kOnce>
-__device__ __forceinline__ void copy_to_lds(const uint8_t* src, uint32_t at, uint32_t lds) {
-  lds = (uint32_t)__builtin_amdgcn_readfirstlane((int)lds);
-  if constexpr (kOnce)
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(at), "s"(src), "s"(lds) : "memory");
-  else
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(at), "s"(src), "s"(lds) : "memory");
-}
-
 // The kinds of pages a sequence's keys come from, in the order they are taken.
 enum Kind { kLowPages = 0, kHighPages = 1, kWindowPages = 2 };
 
