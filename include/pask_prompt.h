@@ -126,10 +126,11 @@ size_t pask_prompt_workspace_bytes(const pask_geom* geom, int32_t batch, int32_t
  * it was persisted, also by queries that are less than W behind it.)
  *
  * Numerics: scores, softmax statistics and sums in fp32, a LOW key enters its
- * score exactly; a softmax weight is rounded once for its product with the value,
- * to bf16 (half a step, 2^-8 of it) where the value is bf16, to fp16 (2^-11, and
- * 2^-33 of the largest) where it is LOW, and its sum is kept of the unrounded
- * ones; a LOW value is rounded once to fp16 (2^-11 of it, whatever else its page
+ * score exactly; a softmax weight is rounded for its product with the value: to
+ * fp16 (half a step, 2^-11 of it, and 2^-33 of the largest) where the value is
+ * LOW, to two bf16 parts (2^-16 is lost, as in pask_decode_attn) where it is bf16
+ * and max_q * n_q_heads / n_kv_heads is at most 32, a draft's call, and to one
+ * bf16 (2^-8) in larger calls; its sum is kept of the unrounded ones; a LOW value is rounded once to fp16 (2^-11 of it, whatever else its page
  * holds); to a LOW key the queries enter as fp16, each row at a power of two
  * that leaves its elements exact down to 2^-28 of the largest.  Weights are taken relative to a reference that a score
  * may exceed by 15 in base 2 before it moves: an output element is certain to be

@@ -228,6 +228,12 @@ __device__ __forceinline__ uint4 packed_weights(const f32x16_t& s, int h) {
   return make_uint4(pack_bf16x2(s[r], s[r + 1]), pack_bf16x2(s[r + 2], s[r + 3]), pack_bf16x2(s[r + 4], s[r + 5]),
                     pack_bf16x2(s[r + 6], s[r + 7]));
 }
+// What packed_weights<false>' rounding left (p: its result), as an operand too: of a weight 2^-16 is lost with both.
+__device__ __forceinline__ uint4 weights_rest(const f32x16_t& s, int h, uint4 p) {
+  const int r = 8 * h;
+  auto two = [&](int x, uint32_t w) { return pack_bf16x2(s[x] - bf16_lo(w), s[x + 1] - bf16_hi(w)); };
+  return make_uint4(two(r, p.x), two(r + 2, p.y), two(r + 4, p.z), two(r + 6, p.w));
+}
 typedef __attribute__((address_space(3))) uint32_t lds_u32;
 __device__ __forceinline__ uint32_t read_lds4(uint32_t lds) { return *(const lds_u32*)(uintptr_t)lds; }
 // N words of LDS, aligned to all of them up to 16 bytes.
@@ -271,8 +277,9 @@ __device__ __forceinline__ void lds_barrier_wave() {
 //   scores  S^T = K Q^T on v_mfma_f32_32x32x16_bf16: a lane holds scores of one
 //           row, so its softmax needs one exchange (with the lane 32 on);
 //   weights online softmax in base 2, rounded once to the type of the values
-//           (bf16: half a step, 2^-8 of a weight); sums are kept of the
-//           unrounded weights;
+//           (bf16: half a step, 2^-8 of a weight; a second product of what that
+//           leaves takes 8,192 bf16 tokens from 538 us to 710); sums are kept of
+//           the unrounded weights;
 //   values  O^T += V^T P^T.
 // Pages lie in the order of 16-row operands; the operands of 32 rows are the
 // same 16-byte chunks of two pages (keys), and 8-byte halves of them (values:
@@ -809,7 +816,10 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
 // next unit's keys asked for once this one's are read, its values likewise; LOW
 // units in two batches, one taken while the other comes.  Eight waves a compute
 // unit (two workgroups) keep up to 128 KiB on its way.  LOW pages are widened in
-// registers.  Numerics are those of prompt_kernel.
+// registers.  Numerics are those of prompt_kernel, but for the weights of bf16
+// values: a draft is verified by these, the decode call's 16 bits of a weight are
+// kept here too, in a second product that costs what reading leaves free (64
+// drafts, bf16 211 -> 213 us, mixed 137 -> 140).
 constexpr int kFewWaves = 4, kFewRows = 32;
 template <int D, int G>
 __global__ __launch_bounds__(64 * kFewWaves, 2) void prompt_few_kernel(PromptArgs a) {
@@ -1124,9 +1134,13 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void prompt_few_kernel(PromptArg
           } else {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              const uint4 p = packed_weights<false>(s, h);
+              const uint4 p = packed_weights<false>(s, h), rest = weights_rest(s, h, p);
 #pragma unroll
-              for (int m = 0; m < VT; ++m) o[m] = mfma(high_value(h, m), p, o[m]);
+              for (int m = 0; m < VT; ++m) {
+                const uint4 v = high_value(h, m);
+                o[m] = mfma(v, p, o[m]);
+                o[m] = mfma(v, rest, o[m]);
+              }
             }
           }
           lds_barrier_wave();
