@@ -76,6 +76,8 @@ __device__ __forceinline__ Keys keys_of(const CacheView& cv, int b, int layer) {
 // take turns begins with the longest, where the sequences are few enough to rank
 // in a wave's lanes (64 drafts behind 1,024-8,192 entries: bf16 235 us in the
 // sequences' own order, 209 so, int4 175 and 139; 16 equal prompts 107 and 111).
+// Larger batches keep their order: 96 drafts take 208 us, 186 where the caller has
+// put the longest first, 96 turns of 4-64 tokens 253 and 198.
 __device__ __forceinline__ int by_length(const PromptArgs& a, int b) {
   if (a.batch == 1 || a.batch > 64 || gridDim.x <= 256) return b;
   const int lane = (int)threadIdx.x & 63;
@@ -140,7 +142,7 @@ struct LowPart {
 // other scales stay as they are (at 1 / 32 the small ones would lose bits), so
 // wide groups have products of their own, between a factor of 1 / 32 and one of
 // 32 on the sums.  That is slow, and rare: 8,192 queries over as many int4 tokens,
-// every scale wide, take 3,580 us where others take 827, 64 drafts 645 and 137.
+// every scale wide, take 3,600 us where others take 827, 64 drafts 432 and 138.
 constexpr uint32_t kWideScale = 0x6954u;
 constexpr float kWide = 32.0f;
 // Of a word's two scales those that are wide, as a mask.
@@ -816,10 +818,10 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
 // next unit's keys asked for once this one's are read, its values likewise; LOW
 // units in two batches, one taken while the other comes.  Eight waves a compute
 // unit (two workgroups) keep up to 128 KiB on its way.  LOW pages are widened in
-// registers.  Numerics are those of prompt_kernel, but for the weights of bf16
-// values: a draft is verified by these, the decode call's 16 bits of a weight are
-// kept here too, in a second product that costs what reading leaves free (64
-// drafts, bf16 211 -> 213 us, mixed 137 -> 140).
+// registers.  Numerics are those of prompt_kernel, but that weights of bf16 values
+// count with 16 bits, as in the decode call that follows a verified draft: a
+// second product, most of it beside the reading (64 drafts behind bf16 histories
+// 227 us without it, 228 with; behind mixed ones 127 and 130).
 constexpr int kFewWaves = 4, kFewRows = 32;
 template <int D, int G>
 __global__ __launch_bounds__(64 * kFewWaves, 2) void prompt_few_kernel(PromptArgs a) {
@@ -972,8 +974,14 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void prompt_few_kernel(PromptArg
           read_words(k0 + L::kLoKS + t16 * 2 * NG, ks);
           read_words(k0 + (g * 16 + t16) * 4 * NG, word0);
           read_words(k0 + ((g + 2) * 16 + t16) * 4 * NG, word1);
-          auto add_keys = [&](int i, uint32_t scales, uint32_t w0, uint32_t w1) __attribute__((always_inline)) {   // group i
-            const uint32_t both = __builtin_amdgcn_perm(scales, scales, i & 1 ? 0x03020302u : 0x01000100u);
+          if (16 * own + t16 >= valid)
+#pragma unroll
+            for (int c = 0; c < NG / 2; ++c) ks[c] = 0u;
+          if (wide_keys)
+#pragma unroll
+            for (int c = 0; c < NG / 2; ++c) ks[c] = scales_of(false, ks[c]);
+          auto add_group = [&](int i, uint32_t sc, uint32_t w0, uint32_t w1) __attribute__((always_inline)) {
+            const uint32_t both = __builtin_amdgcn_perm(sc, sc, i & 1 ? 0x03020302u : 0x01000100u);
             const f16x2_t s8 = halves(both & 0xFFF8FFF8u), s3 = halves(both) - s8;
 #pragma unroll
             for (int w = 0; w < 2; ++w) {          // quarters g and g + 2: chunks 2 (2 i + w) + g
@@ -982,26 +990,20 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void prompt_few_kernel(PromptArg
               s = mfma_half(key_part(word, s3), qf[2 * i + w], s);
             }
           };
-          if (!wide_keys) {
-            if (16 * own + t16 >= valid)
 #pragma unroll
-              for (int c = 0; c < NG / 2; ++c) ks[c] = 0u;
+          for (int i = 0; i < NG; ++i) add_group(i, ks[i / 2], word0[i], word1[i]);
+          if (wide_keys) {
+            s *= 1.0f / kWide;
+            const int l = fresh(lane), t = l & 15;
+            const uint32_t at = low0 + (l >> 4 & 1) * L::kLoHead;
 #pragma unroll
-            for (int i = 0; i < NG; ++i) add_keys(i, ks[i / 2], word0[i], word1[i]);
-          } else {
-#pragma unroll 1
-            for (int wide = 0; wide < 2; ++wide) { // the groups that are not wide, then those that are
-              const int l = fresh(lane), t = l & 15;
-              const uint32_t at = low0 + (l >> 4 & 1) * L::kLoHead;
-#pragma unroll
-              for (int i = 0; i < NG; ++i) {
-                const uint32_t scales = (l & 31) < valid ? scales_of(wide != 0, read_lds4(at + L::kLoKS + t * 2 * NG + 4 * (i / 2))) : 0u;
-                const uint32_t word = at + ((l >> 5) * 16 + t) * 4 * NG + 4 * i;
-                add_keys(i, scales, read_lds4(word), read_lds4(word + 128 * NG));
-                __builtin_amdgcn_sched_barrier(0);
-              }
-              s *= wide ? kWide : 1.0f / kWide;
+            for (int i = 0; i < NG; ++i) {
+              const uint32_t sc = (l & 31) < valid ? scales_of(true, read_lds4(at + L::kLoKS + t * 2 * NG + 4 * (i / 2))) : 0u;
+              const uint32_t word = at + ((l >> 5) * 16 + t) * 4 * NG + 4 * i;
+              add_group(i, sc, read_lds4(word), read_lds4(word + 128 * NG));
+              __builtin_amdgcn_sched_barrier(0);
             }
+            s *= kWide;
           }
         } else {
           const uint32_t k0 = fresh(room + own * kPart + g * 256 + t16 * 16);
@@ -1056,38 +1058,39 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void prompt_few_kernel(PromptArg
           }
         }
         if constexpr (kLow) {
-          if (!wide_values) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              uint32_t v[VT][4];
+          for (int h = 0; h < 2; ++h) {
+            uint32_t v[VT][4];
 #pragma unroll
-              for (int w = 0; w < 2; ++w) {        // slots 4 g .. and 4 g + 8 .., the parity's nibbles
-                uint32_t vs[2 * NG], code[NG];
-                read_words(low0 + h * L::kLoHead + L::kLoVS + (g + 2 * w) * 8 * NG, vs);
-                read_words(low0 + h * L::kLoHead + L::kLoVC + ((g + 2 * w) * 16 + t16) * 4 * NG, code);
-                if (valid < 32)
+            for (int w = 0; w < 2; ++w) {          // slots 4 g .. and 4 g + 8 .., the parity's nibbles
+              uint32_t vs[2 * NG], code[NG];
+              read_words(low0 + h * L::kLoHead + L::kLoVS + (g + 2 * w) * 8 * NG, vs);
+              read_words(low0 + h * L::kLoHead + L::kLoVC + ((g + 2 * w) * 16 + t16) * 4 * NG, code);
+              if (valid < 32)
 #pragma unroll
-                  for (int c = 0; c < 2 * NG; ++c)
-                    if (16 * h + 4 * (g + 2 * w) + c / (NG / 2) >= valid) vs[c] = 0u;
+                for (int c = 0; c < 2 * NG; ++c)
+                  if (16 * h + 4 * (g + 2 * w) + c / (NG / 2) >= valid) vs[c] = 0u;
+              if (wide_values)
 #pragma unroll
-                for (int m = 0; m < VT; ++m) {
-                  const uint32_t pick = m & 1 ? 0x07060302u : 0x05040100u;
+                for (int c = 0; c < 2 * NG; ++c) vs[c] = scales_of(false, vs[c]);
 #pragma unroll
-                  for (int t = 0; t < 2; ++t)
-                    v[m][2 * w + t] = word_of(code_pair(code[m] >> (4 * own), t) *
-                                              halves(__builtin_amdgcn_perm(vs[(t + 2) * (NG / 2) + m / 2], vs[t * (NG / 2) + m / 2], pick)));
-                }
+              for (int m = 0; m < VT; ++m) {
+                const uint32_t pick = m & 1 ? 0x07060302u : 0x05040100u;
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+                  v[m][2 * w + t] = word_of(code_pair(code[m] >> (4 * own), t) *
+                                            halves(__builtin_amdgcn_perm(vs[(t + 2) * (NG / 2) + m / 2], vs[t * (NG / 2) + m / 2], pick)));
               }
-              const uint4 p = packed_weights<true>(s, h);
-#pragma unroll
-              for (int m = 0; m < VT; ++m) o[m] = mfma_half(make_uint4(v[m][0], v[m][1], v[m][2], v[m][3]), p, o[m]);
             }
-          } else {
+            const uint4 p = packed_weights<true>(s, h);
+#pragma unroll
+            for (int m = 0; m < VT; ++m) o[m] = mfma_half(make_uint4(v[m][0], v[m][1], v[m][2], v[m][3]), p, o[m]);
+          }
+          if (wide_values) {
             const uint4 p0 = packed_weights<true>(s, 0), p1 = packed_weights<true>(s, 1);
 #pragma unroll 1
-            for (int x = 0; x < 4; ++x) {          // both pages' groups that are not wide, then those that are
-              const int h = x & 1, l = fresh(lane), slot_at = 16 * h + 4 * (l >> 5);
-              const bool wide = x >= 2;
+            for (int h = 0; h < 2; ++h) {
+              const int l = fresh(lane), first_slot = 16 * h + 4 * (l >> 5);
               const uint4 p = make_uint4(h ? p1.x : p0.x, h ? p1.y : p0.y, h ? p1.z : p0.z, h ? p1.w : p0.w);
               const uint32_t scales = low0 + h * L::kLoHead + L::kLoVS + (l >> 5) * 8 * NG;
               const uint32_t codes = low0 + h * L::kLoHead + L::kLoVC + ((l >> 5) * 16 + (l & 15)) * 4 * NG;
@@ -1095,17 +1098,18 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void prompt_few_kernel(PromptArg
               for (int m = 0; m < VT; ++m) {
                 uint32_t v[4];
 #pragma unroll
-                for (int y = 0; y < 4; ++y) {      // slots t and t + 2
+                for (int y = 0; y < 4; ++y) {      // slots t and t + 2 of four
                   const int w = y >> 1, t = y & 1;
                   auto scale_at = [&](int z) {
-                    return slot_at + 8 * w + z < valid ? scales_of(wide, read_lds4(scales + 16 * w * NG + z * 2 * NG + 4 * (m / 2))) : 0u;
+                    const uint32_t sc = read_lds4(scales + 16 * w * NG + z * 2 * NG + 4 * (m / 2));
+                    return first_slot + 8 * w + z < valid ? scales_of(true, sc) : 0u;
                   };
-                  const uint32_t code = read_lds4(codes + w * 128 * NG + 4 * m);
-                  v[y] = word_of(code_pair(code >> (l >> 2 & 4), t) *
+                  v[y] = word_of(code_pair(read_lds4(codes + w * 128 * NG + 4 * m) >> (l >> 2 & 4), t) *
                                  halves(__builtin_amdgcn_perm(scale_at(t + 2), scale_at(t), m & 1 ? 0x07060302u : 0x05040100u)));
                 }
+                if (h == 0) o[m] *= 1.0f / kWide;
                 o[m] = mfma_half(make_uint4(v[0], v[1], v[2], v[3]), p, o[m]);
-                if (h) o[m] *= wide ? kWide : 1.0f / kWide;
+                if (h == 1) o[m] *= kWide;
                 __builtin_amdgcn_sched_barrier(0);
               }
             }
@@ -1128,19 +1132,21 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void prompt_few_kernel(PromptArg
               wild |= abs_max_bits8(v) >= 0x7F80u;
             }
           }
-          if (__ballot(wild)) {
+          if (__ballot(wild)) {                    // key by key, which leaves nothing for the products
             const uint8_t* values = s_room[wave] + 2 * kPart;
             add_seen_values<VT>(values, values + kPart, s, hidden, o, g, n);
-          } else {
+            lds_barrier_wave();
+#pragma unroll 1
+            for (int c = 0; c < kHalf; ++c) write_lds16(room + 2 * kPart + lane * 16 + c * 1024, make_uint4(0u, 0u, 0u, 0u));
+          }
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const uint4 p = packed_weights<false>(s, h), rest = weights_rest(s, h, p);
+          for (int h = 0; h < 2; ++h) {
+            const uint4 p = packed_weights<false>(s, h), rest = weights_rest(s, h, p);
 #pragma unroll
-              for (int m = 0; m < VT; ++m) {
-                const uint4 v = high_value(h, m);
-                o[m] = mfma(v, p, o[m]);
-                o[m] = mfma(v, rest, o[m]);
-              }
+            for (int m = 0; m < VT; ++m) {
+              const uint4 v = high_value(h, m);
+              o[m] = mfma(v, p, o[m]);
+              o[m] = mfma(v, rest, o[m]);
             }
           }
           lds_barrier_wave();
@@ -1327,12 +1333,12 @@ void launch_dim(const PromptArgs& a, const PromptCut& c, hipStream_t s) {
 
 // Tiles of 256 rows, whose eight waves share every page through LDS, or of 32,
 // whose waves share the rows, where no sequence has more (32 sequences of 1,000-
-// 8,000 tokens, 32 rows of each: 82 us so, 150 in tiles of 256; 48 rows, in a build
+// 8,000 tokens, 32 rows of each: 79 us so, 145 in tiles of 256; 48 rows, in a build
 // before, in two tiles of 32: 153, in one of 256: 155).  The keys are cut into
 // pieces where the tiles leave compute units idle: for 32 rows by the workgroups the
 // card holds (8 KV heads; with 1, 2 and 4 pieces 128 sequences of 500-4,096 tokens
-// take 134, 147, 159 us, 64 of 1,024-8,192 124, 124, 140, 32 of 1,000-8,000 97, 82,
-// 81; one of 32,005 tokens with 32, 64 and 128 pieces 31, 29, 43).  For tiles of 256
+// take 131, 142, 155 us, 64 of 1,024-8,192 124, 130, 140, 32 of 1,000-8,000 94, 78,
+// 78; one of 32,005 tokens with 32, 64 and 128 pieces 29, 27, 41).  For tiles of 256
 // rows by what a call takes with each number of pieces, in microseconds: as many
 // turns of the 256 compute units as the workgroups need, each a piece's steps at
 // 2.5 (64 keys: 2.1 of bf16 pages, 3.2 of int4 ones) and 10 to begin and end, and
