@@ -71,3 +71,15 @@ def test_more_pieces_than_a_round_of_the_joining(D, n):
     r.append([n])
     r.attend([3], what="pieces")
     r.attend([3], first=[n // 2], what="pieces, in the middle")
+
+
+@pytest.mark.parametrize("Hq, Hkv, n_q, n", [(8, 2, 3, 40), (8, 2, 3, 1900), (8, 8, 100, 300), (8, 1, 100, 2900)])
+def test_outputs_may_take_the_queries_place(Hq, Hkv, n_q, n):
+    """Few and many rows, with one piece and with more: a workgroup writes rows that it alone reads, after reading them."""
+    r = Run(2, Hq, Hkv, 128, 3000, MIXED, window=9, seed=n + n_q)
+    r.append([n, n // 2 + n_q])
+    q = normal(r.gen, 2, n_q, Hq, 128).cuda()
+    out = torch.empty_like(q)
+    r.s.prompt(0, q, out, max_ctx_hint=n)
+    r.s.prompt(0, q, q, max_ctx_hint=n)
+    assert torch.equal(q.view(torch.int16), out.view(torch.int16))
