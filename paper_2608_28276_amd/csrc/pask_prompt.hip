@@ -821,7 +821,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
 // registers.  Numerics are those of prompt_kernel, but that weights of bf16 values
 // count with 16 bits, as in the decode call that follows a verified draft: a
 // second product, most of it beside the reading (64 drafts behind bf16 histories
-// 227 us without it, 228 with; behind mixed ones 127 and 130).
+// 227 us without it and with it; behind mixed ones 127 and 129).
 constexpr int kFewWaves = 4, kFewRows = 32;
 template <int D, int G>
 __global__ __launch_bounds__(64 * kFewWaves, 2) void prompt_few_kernel(PromptArgs a) {
@@ -1139,15 +1139,23 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void prompt_few_kernel(PromptArg
 #pragma unroll 1
             for (int c = 0; c < kHalf; ++c) write_lds16(room + 2 * kPart + lane * 16 + c * 1024, make_uint4(0u, 0u, 0u, 0u));
           }
+          // Operands read four ahead, in pinned order: two reads that the compiler merges cost more than one after the other.
+          uint4 v[kAhead], p = make_uint4(0u, 0u, 0u, 0u), rest = p;
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const uint4 p = packed_weights<false>(s, h), rest = weights_rest(s, h, p);
+          for (int x = 0; x < kAhead; ++x) {
+            v[x] = high_value(x / VT, x % VT);
+            __builtin_amdgcn_sched_barrier(0);
+          }
 #pragma unroll
-            for (int m = 0; m < VT; ++m) {
-              const uint4 v = high_value(h, m);
-              o[m] = mfma(v, p, o[m]);
-              o[m] = mfma(v, rest, o[m]);
+          for (int x = 0; x < 2 * VT; ++x) {
+            if (x % VT == 0) {
+              p = packed_weights<false>(s, x / VT);
+              rest = weights_rest(s, x / VT, p);
             }
+            o[x % VT] = mfma(v[x % kAhead], p, o[x % VT]);
+            o[x % VT] = mfma(v[x % kAhead], rest, o[x % VT]);
+            if (x + kAhead < 2 * VT) v[x % kAhead] = high_value((x + kAhead) / VT, (x + kAhead) % VT);
+            __builtin_amdgcn_sched_barrier(0);
           }
           lds_barrier_wave();
           if (next < to) copy_half(next, 1);
