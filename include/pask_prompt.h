@@ -42,7 +42,9 @@ enum {
   PASK_ROPE_PARTS = 3         /* g theta_i + (1 - g) theta_i / factor, g rising
                                  from 0 to 1 as the turns of pair i over
                                  original_len positions go from low_turns to
-                                 high_turns */
+                                 high_turns (not a ramp over i between two
+                                 rounded pairs: its frequencies are written
+                                 into turns) */
 };
 
 /* A rotation: plain data, filled by pask_rope_init.  Passed by value to the
@@ -136,7 +138,9 @@ size_t pask_prompt_workspace_bytes(const pask_geom* geom, int32_t batch, int32_t
  * may exceed by 15 in base 2 before it moves: an output element is certain to be
  * finite where the query's scores and the sums they are made of are finite in
  * fp32 and the magnitudes of its values, over the entries seen, sum to less than
- * 2^112.
+ * 2^112.  A score of -Inf has weight 0 beside finite ones; one of +Inf or NaN makes
+ * its query NaN; a value that is not finite reaches its own element of the queries
+ * that see it, which are not finite there.
  *
  * ws_dev: device workspace of at least pask_prompt_workspace_bytes(geom, batch,
  * max_q, max_ctx_hint) bytes, 256-byte aligned (ignored where that is 0); calls

@@ -109,3 +109,21 @@ def test_values_reach_their_own_element(D, n_q, window, value):
             assert np.isnan(got).all() if np.isnan(value) else (got == value).all(), got
             out[m:, h, 7] = want[m:, 7]
         check(out[:, h], want, tol, f"out of head {h}")
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n_q", [4, 120])
+@pytest.mark.parametrize("value", [INF, -INF, NAN])
+@pytest.mark.parametrize("at", [0, 100])
+def test_values_that_all_queries_see_reach_their_own_element(D, n_q, value, at):
+    """Among whole steps of keys: that element of the heads that read it is not finite, every other one exact."""
+    k, v, q = tensors(D + n_q + 3, D, n_q)
+    v[0, at, 1, 7] = value
+    out, lse = (b := Both(D, k, v)).run(q)
+    for h in range(4):
+        want, want_lse, tol, lse_tol = b.want(q, h)
+        check(lse[:, h], want_lse, lse_tol, f"lse of head {h}")
+        if h >= 2:
+            assert not np.isfinite(out[:, h, 7]).any()
+            out[:, h, 7] = want[:, 7]
+        check(out[:, h], want, tol, f"out of head {h}")
