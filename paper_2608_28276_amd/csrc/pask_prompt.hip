@@ -308,7 +308,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
   constexpr int kPart = L::kHiV, kValues = 2 * kPart, kTile = 3 * kPart, kStep = kStepPages * kTile;
   __shared__ __align__(1024) uint8_t s_kv[3][kStep];
   // LOW parts (keys, values of a page) with a wide scale; of those, which slots' scale is, for each group.
-  __shared__ __align__(16) uint32_t s_wide[3][2 * kStepPages], s_wide_slots[3][2 * kStepPages][NG];
+  __shared__ __align__(16) uint32_t s_wide[3 * 2 * kStepPages], s_wide_slots[3 * 2 * kStepPages][NG];
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int g = lane >> 5, n = lane & 31;
   // Workgroups go to the 8 XCDs in turn: neighbours are different KV heads.  The
@@ -450,7 +450,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
           } else {                                 // lane t's slot t
             of = (uint32_t)__ballot(of != 0u) & 0xFFFFu;
           }
-          if (lane == 0) s_wide_slots[j % 3][x][i] = of;
+          if (lane == 0) s_wide_slots[2 * kStepPages * (j % 3) + x][i] = of;
         }
 #pragma unroll
         for (int c = 0; c < 2 * NG; ++c) {
@@ -458,7 +458,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
           sc[c] = (at_1_32(sc[c]) & m) | (sc[c] & ~m);
         }
       }
-      if (lane == 0) s_wide[j % 3][x] = wide;
+      if (lane == 0) s_wide[2 * kStepPages * (j % 3) + x] = wide;
       const uint32_t at = dst + p * kTile + (values ? kValues : 0) + lane * 16;
       if (values) {
 #pragma unroll
@@ -536,9 +536,10 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
     for (int r = 0; r < 16; ++r) s[r] = 0.0f;
 #pragma unroll 1
     for (int wide = 0; wide < 2; ++wide) {
-      const int l = fresh(lane), part = 8 * slot + 4 * (i & 1) + 2 * (l >> 4 & 1);   // the keys of the page of the lane's slot
-      const uint32_t ks = fresh(unit_at(slot, i) + k_at), some = (&s_wide[0][0])[part] ? 1u << (l & 15) : 0u;
-      const uint32_t* slots_of = s_wide_slots[0][part];
+      const int l = fresh(lane);                   // the part: keys of the page of the lane's slot
+      const int part = 2 * kStepPages * slot + 4 * (i & 1) + 2 * (l >> 4 & 1);
+      const uint32_t ks = fresh(unit_at(slot, i) + k_at), some = s_wide[part] ? 1u << (l & 15) : 0u;
+      const uint32_t* slots_of = s_wide_slots[part];
 #pragma unroll
       for (int k = 0; k < 2 * KI; ++k) {
         const uint32_t take = ((slots_of[k / 4] & some) != 0u) == (wide != 0) ? ~0u : 0u;
@@ -569,7 +570,8 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
   // The weights' base: 0 while every score was -Inf (their weights are 0, and -Inf - -Inf is not).
   auto base_of_weights = [&] { return mx == -INFINITY ? 0.0f : mx; };
   auto any_wide = [&](int s) {
-    const uint4 x = *reinterpret_cast<const uint4*>(s_wide[s]), y = *reinterpret_cast<const uint4*>(s_wide[s] + 4);
+    const uint4* parts = reinterpret_cast<const uint4*>(s_wide + 2 * kStepPages * s);
+    const uint4 x = parts[0], y = parts[1];
     return __builtin_amdgcn_readfirstlane((int)(x.x | x.y | x.z | x.w | y.x | y.y | y.z | y.w)) != 0;
   };
 
@@ -685,7 +687,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
           const int k = slot0 + 8 * (r >> 2) + 4 * g + (r & 3);
           return ring ? !in || ring_position(keys, a.cv.window, k) > at : k >= sees;
         };
-        const uint32_t* wide_parts = &s_wide[slot][4 * (i & 1)];   // keys, values of the unit's two pages
+        const uint32_t* wide_parts = &s_wide[2 * kStepPages * slot + 4 * (i & 1)];   // keys, values of the unit's two pages
         const bool wide_keys = decltype(is_low)::value && __builtin_amdgcn_readfirstlane((int)(wide_parts[0] | wide_parts[2]));
         if (__builtin_expect(wide_keys, 0)) s = wide_scores(i);
         else s = scores(is_low, i);
@@ -713,7 +715,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void prompt_kernel(PromptArgs a) {
 #pragma unroll 1
             for (int wide = 0; wide < 2; ++wide) {
               const uint32_t at0 = fresh(vs), at1 = fresh(vs + 512);
-              const uint32_t* slots_of = s_wide_slots[0][fresh(8 * slot + 4 * (i & 1) + 2 * h + 1)];
+              const uint32_t* slots_of = s_wide_slots[fresh(2 * kStepPages * slot + 4 * (i & 1) + 2 * h + 1)];
               const int t = fresh(4 * g);
 #pragma unroll
               for (int m = 0; m < VT; ++m) {       // dimensions of group m: the weights of the slots that are wide there, or not
